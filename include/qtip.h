@@ -293,6 +293,105 @@ int qtip_quantize_ldlq(const float *W, const float *A, int m, int n, int L, int 
                        const void *lut_f16, uint32_t *codes_out, float *What_out, float *tile_err,
                        void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * 8-BIT LAYERS, AND WHAT STANDS AROUND A LAYER
+ *
+ * A model whose large layers are trellis coded keeps some in 8 bits, and has norms, residual sums and
+ * perhaps experts between them.  Formats shared by the calls below (device memory all):
+ *   type    of values: QTIP_F16, QTIP_BF16 (the upper half of a binary32), QTIP_F32, QTIP_I8.
+ *   ld...   how many values apart the rows of a matrix begin (at least as many as are used); int64.
+ *           Rows may begin at any address that their type allows unless a call asks for more.
+ *   8 bits  a row (of weights or activations) is int8 values and one fp32 scale; the value is their product.
+ */
+#define QTIP_F16 0
+#define QTIP_BF16 1
+#define QTIP_F32 2
+#define QTIP_I8 3
+
+#define QTIP_ROWS_MAX_N 32768 /* longest row of the calls that hold one in registers */
+#define QTIP_I8_MAX_N 131071  /* most inputs of an 8-bit product: n 128^2 stays below 2^31 */
+#define QTIP_I8_MAX_B (65535 * 16)
+
+/*
+ * Rows to 8 bits: for each of `rows` rows of n values
+ *     v = x, or silu(x) .* up where up is not NULL (silu(t) = t / (1 + exp(-t)));
+ *     v = V (S .* v) where signs is not NULL, as qtip_rht side 0 with the same block;
+ *     a = max |v|;  scale = a / 127;  q = v (127 / a) rounded to the nearest whole number, ties to even.
+ * q is in [-127, 127].  A row of zeros has scale 0; a row with an infinity or a NaN has
+ * scale NaN (and q = 0), so that what is computed from it is NaN, not a finite number.
+ * Arithmetic is fp32.  Applied with the same signs and block to the rows of a weight matrix and to
+ * activations it gives both sides of a rotated 8-bit layer (W x = (W S V^T)(V S x)): no
+ * transform is needed behind the product.
+ *   x, up: rows ldx apart, of `type` (F16, BF16, F32).  signs: n int8 of +1 and -1, 4-byte aligned, or NULL (block is
+ *   ignored then); n a multiple of block, block a power of two in [16, 16384].  q: rows ldq apart (bytes between a
+ *   row's n-th and the next row are left alone).  scale: `rows` fp32.  n at most QTIP_ROWS_MAX_N.
+ */
+int qtip_quantize_rows_i8(const void *x, const void *up, int type, int rows, int n, int64_t ldx, const int8_t *signs, int block,
+                          int8_t *q, int64_t ldq, float *scale, void *stream);
+
+/*
+ * The product of 8-bit rows with 8-bit weights, a scale for each row of either:
+ *     Y[b][i] = w_scale[i] x_scale[b] (sum_j W[i][j] X[b][j]) + bias[i],   i < m, j < n, b < B.
+ * The sum is exact (32-bit whole numbers); scales, bias and their sum are fp32, rounded once to y_type.
+ *   W: m rows, X: B rows; both begin at multiples of 16 bytes (ldw and ldx are multiples of 16, so a row may be any n
+ *   long; up to 15 bytes behind its end are read and count for nothing).  w_scale: m, x_scale: B, bias: m fp32 or NULL.
+ *   Y: rows ldy apart, of y_type (F16, BF16, F32).  n at most QTIP_I8_MAX_N, B at most QTIP_I8_MAX_B.
+ *   workspace: qtip_matmul_i8_workspace(m, n, B) bytes, 256-byte aligned; NULL where that is 0.  Contents are scratch.
+ */
+size_t qtip_matmul_i8_workspace(int m, int n, int B);
+int qtip_matmul_i8(const int8_t *W, int64_t ldw, const float *w_scale, int m, int n, const int8_t *X, int64_t ldx,
+                   const float *x_scale, int B, const float *bias, void *Y, int64_t ldy, int y_type, void *workspace,
+                   size_t workspace_bytes, void *stream);
+
+/*
+ * What stands between two blocks, in one launch: for each row
+ *     a = y, or post(y) where post_weight is not NULL;    the norm behind the block
+ *     a = gate .* a where gate is not NULL;
+ *     h' = h + res_scale a  (without h: res_scale a; without y: h);         stored as h_out
+ *     x = h', or pre(h') where pre_weight is not NULL;    the norm in front of the next block
+ *     x = V (S .* x) where signs is not NULL, as qtip_rht side 0;           stored as x
+ * post and pre are norms of one kind:
+ *     QTIP_NORM_RMS    v / sqrt(mean(v^2) + eps) .* weight + bias
+ *     QTIP_NORM_LAYER  (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) .* weight + bias
+ * Arithmetic is fp32 on fp32 values: x is made of h' before its rounding.
+ *   y, gate: of y_type (F16, BF16, F32).  h, h_out: of h_type, the same or F32, rows of both ldh apart; h_out may be h
+ *   (and may be NULL).  ldgate = 0: one row for all (a scale per channel).  weights and biases: n fp32; a bias may be
+ *   NULL.  x: of x_type, also I8 (then with x_scale, `rows` fp32, exactly as qtip_quantize_rows_i8 makes it), or NULL.
+ *   signs, block: as qtip_quantize_rows_i8; x in F16 is then what qtip_decode_matvec and qtip_decode_matmat take.
+ */
+#define QTIP_NORM_RMS 0
+#define QTIP_NORM_LAYER 1
+int qtip_norm_residual(const void *y, int64_t ldy, int y_type, const void *h, int64_t ldh, int h_type, const void *gate,
+                       int64_t ldgate, int rows, int n, int norm, const float *post_weight, const float *post_bias,
+                       const float *pre_weight, const float *pre_bias, float eps, float res_scale, const int8_t *signs,
+                       int block, void *h_out, void *x, int64_t ldx, int x_type, float *x_scale, void *stream);
+
+/*
+ * A mixture-of-experts layer for up to QTIP_MOE_MAX_TOKENS tokens: for each row x
+ *     l = R x + router_bias;  the top_k experts with the largest l, ties to the lowest expert;
+ *     p = softmax(l) over all E experts, or over the chosen ones where renormalize is not 0;
+ *     g = G_e x,  u = U_e x,  y = sum over the chosen e of p_e D_e (silu(g) .* u).
+ * The experts' weights are 8-bit rows (as qtip_quantize_rows_i8 makes them), activations stay in 16 bits (the weights'
+ * bytes are what a few tokens wait for); products, softmax and sums are fp32, y is rounded once.
+ * Every chosen expert's weights are read once.
+ *   x, y: T rows of n, ldx and ldy values apart, of `type` (F16, BF16); x 16-byte aligned, ldx a multiple of 8; y not x.
+ *   router: E x n of `type`.  router_bias: E fp32 or NULL; -infinity masks an expert.  A masked expert that is chosen for
+ *   want of others has weight 0 and is left out; a token without any expert gets y = 0.  A NaN among a token's logits
+ *   (a NaN in its x) makes all its weights NaN.
+ *   W_up: E x 2f x n int8, an expert's rows of G, then those of U; up_scale: E x 2f fp32.  W_down: E x n x f int8;
+ *   down_scale: E x n fp32.  n and f: multiples of 16, at most QTIP_ROWS_MAX_N.  All 16-byte aligned.
+ *   ids: T x top_k int32, weights: T x top_k fp32, by descending l: the choice and p; either may be NULL.
+ *   workspace: qtip_moe_i8_workspace(T, n, f, E, top_k) bytes, 256-byte aligned; contents are scratch.
+ */
+#define QTIP_MOE_MAX_TOKENS 64
+#define QTIP_MOE_MAX_EXPERTS 256
+#define QTIP_MOE_MAX_TOP_K 16
+size_t qtip_moe_i8_workspace(int T, int n, int f, int E, int top_k);
+int qtip_moe_i8(const void *x, int64_t ldx, int type, int T, int n, const void *router, const float *router_bias, int E,
+                int top_k, int renormalize, const int8_t *W_up, const float *up_scale, int f, const int8_t *W_down,
+                const float *down_scale, void *y, int64_t ldy, int32_t *ids, float *weights, void *workspace,
+                size_t workspace_bytes, void *stream);
+
 /* Message for the last error on this thread ("" if none). Never NULL. */
 const char *qtip_last_error(void);
 

@@ -13,6 +13,10 @@ import numpy as np
 
 CODE_1MAD, CODE_3INST, CODE_HYB, CODE_HYB2, CODE_LUT, CODE_HYB1 = 0, 1, 2, 3, 4, 5
 
+# types of values, and norms
+F16, BF16, F32, I8 = 0, 1, 2, 3
+NORM_RMS, NORM_LAYER = 0, 1
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 # The environment variable QTIP_LIBRARY names another build of the same library to load instead
 # (two builds compared on one box; the sanitizer build of the host code in tests/test_sanitizers.py).
@@ -24,7 +28,8 @@ EXPORTS = ["qtip_rht", "qtip_rht_f32", "qtip_decode_matvec", "qtip_rht_decode_ma
            "qtip_dequantize", "qtip_decode_states", "qtip_quantize",
            "qtip_quantize_gpu_workspace", "qtip_quantize_gpu", "qtip_block_ldl_workspace",
            "qtip_block_ldl", "qtip_quantize_ldlq_workspace", "qtip_quantize_ldlq", "qtip_last_error",
-           "qtip_version"]
+           "qtip_version", "qtip_quantize_rows_i8", "qtip_matmul_i8_workspace", "qtip_matmul_i8", "qtip_norm_residual",
+           "qtip_moe_i8_workspace", "qtip_moe_i8"]
 
 
 class QtipError(RuntimeError):
@@ -87,6 +92,18 @@ def lib():
         L.qtip_quantize_ldlq.restype = i32
         L.qtip_quantize_ldlq.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp,
                                          c.c_size_t, vp]
+        i64, f32, size = c.c_int64, c.c_float, c.c_size_t
+        for name, result, arguments in [
+                ("qtip_quantize_rows_i8", i32, [vp, vp, i32, i32, i32, i64, vp, i32, vp, i64, vp, vp]),
+                ("qtip_matmul_i8_workspace", size, [i32, i32, i32]),
+                ("qtip_matmul_i8", i32, [vp, i64, vp, i32, i32, vp, i64, vp, i32, vp, vp, i64, i32, vp, size, vp]),
+                ("qtip_norm_residual", i32, [vp, i64, i32, vp, i64, i32, vp, i64, i32, i32, i32, vp, vp, vp, vp, f32, f32,
+                                             vp, i32, vp, vp, i64, i32, vp, vp]),
+                ("qtip_moe_i8_workspace", size, [i32, i32, i32, i32, i32]),
+                ("qtip_moe_i8", i32, [vp, i64, i32, i32, i32, vp, vp, i32, i32, i32, vp, vp, i32, vp, vp, vp, i64, vp, vp,
+                                      vp, size, vp])]:
+            if hasattr(L, name):  # (QTIP_LIBRARY may name a build without them)
+                getattr(L, name).restype, getattr(L, name).argtypes = result, arguments
         _lib = L
     return _lib
 
@@ -128,13 +145,15 @@ def _check(rc):
 _GPU_ENTRIES = ["qtip_rht", "qtip_rht_f32", "qtip_decode_matvec", "qtip_rht_decode_matvec",
                 "qtip_rht_decode_matvec_noalloc", "qtip_decode_matmat", "qtip_dequantize", "qtip_decode_states",
                 "qtip_quantize_gpu", "qtip_block_ldl", "qtip_quantize_ldlq"]
+# Those of 8-bit layers and of what stands around a layer.
+_LAYER_ENTRIES = ["qtip_quantize_rows_i8", "qtip_matmul_i8", "qtip_norm_residual", "qtip_moe_i8"]
 _call = None
 
 
 def _connect():
     """Give the entry points of _call the addresses of the loaded library's functions."""
     L = lib()
-    for name in _GPU_ENTRIES:
+    for name in _GPU_ENTRIES + [name for name in _LAYER_ENTRIES if hasattr(L, name)]:
         _call.connect(getattr(_call, name), ctypes.cast(getattr(L, name), ctypes.c_void_p).value)
 
 
@@ -227,6 +246,28 @@ def qtip_quantize_ldlq(W, A, m, n, L, k, V, code_id, lut, codes_out, What_out, t
     """A weight matrix to code streams with feedback (BlockLDLQ)."""
 
 
+@_entry
+def qtip_quantize_rows_i8(x, up, type, rows, n, ldx, signs, block, q, ldq, scale, stream=None):
+    """Rows (silu(x) .* up with up; V (S .* v) with signs) to int8 with an fp32 scale each."""
+
+
+@_entry
+def qtip_matmul_i8(W, ldw, w_scale, m, n, X, ldx, x_scale, B, bias, Y, ldy, y_type, workspace, workspace_bytes, stream=None):
+    """Y[b] = w_scale .* (W X[b]) x_scale[b] + bias of 8-bit weights and rows."""
+
+
+@_entry
+def qtip_norm_residual(y, ldy, y_type, h, ldh, h_type, gate, ldgate, rows, n, norm, post_weight, post_bias, pre_weight,
+                       pre_bias, eps, res_scale, signs, block, h_out, x, ldx, x_type, x_scale, stream=None):
+    """h_out = h + res_scale gate .* post(y); x = pre(h_out), rotated with signs, in x_type (int8 with x_scale)."""
+
+
+@_entry
+def qtip_moe_i8(x, ldx, type, T, n, router, router_bias, E, top_k, renormalize, W_up, up_scale, f, W_down, down_scale, y, ldy,
+                ids, weights, workspace, workspace_bytes, stream=None):
+    """A mixture-of-experts layer with 8-bit experts for up to 64 tokens."""
+
+
 def qtip_version():
     return int(lib().qtip_version())
 
@@ -261,3 +302,9 @@ def qtip_quantize_ldlq_workspace(m, n, k, V, tiles):
     return int(lib().qtip_quantize_ldlq_workspace(m, n, k, V, tiles))
 
 
+def qtip_matmul_i8_workspace(m, n, B):
+    return int(lib().qtip_matmul_i8_workspace(m, n, B))
+
+
+def qtip_moe_i8_workspace(T, n, f, E, top_k):
+    return int(lib().qtip_moe_i8_workspace(T, n, f, E, top_k))

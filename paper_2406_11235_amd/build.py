@@ -10,8 +10,9 @@ LIB = os.path.join(HERE, "libqtip.so")
 # (with the interpreter's tag: _call is built for one Python, and another one may not load it)
 CALL = os.path.join(HERE, "_call" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 CALL_SOURCE = os.path.join(CSRC, "qtip_call.cpp")
-SOURCES = ["qtip_api.hip", "qtip_decode.hip", "qtip_lut14.hip", "qtip_gemm.hip", "qtip_rht.hip", "qtip_viterbi.hip", "qtip_ldlq.hip", "qtip_quantize.cpp"]
-HEADERS = ["qtip_device.h", "qtip_rht_device.h", "qtip_internal.h", os.path.join("..", "..", "include", "qtip.h")]
+SOURCES = ["qtip_api.hip", "qtip_decode.hip", "qtip_lut14.hip", "qtip_gemm.hip", "qtip_rht.hip", "qtip_viterbi.hip", "qtip_ldlq.hip", "qtip_quantize.cpp",
+           "qtip_api_i8.hip", "qtip_rows.hip", "qtip_i8.hip", "qtip_moe.hip"]
+HEADERS = ["qtip_device.h", "qtip_rht_device.h", "qtip_rows_device.h", "qtip_internal.h", os.path.join("..", "..", "include", "qtip.h")]
 
 # Packed-FP32 VALU forms are switched off for every device compile.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-pthread",

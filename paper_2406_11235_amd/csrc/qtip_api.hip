@@ -9,13 +9,9 @@
 #include "../../include/qtip.h"
 #include "qtip_internal.h"
 
-namespace {
+namespace qtip {
 
-bool is_hyb(int code_id) { return code_id == QTIP_CODE_HYB || code_id == QTIP_CODE_HYB2; }
-bool is_lut(int code_id) { return code_id == QTIP_CODE_LUT; }
-bool has_table(int code_id) { return is_hyb(code_id) || is_lut(code_id) || code_id == QTIP_CODE_HYB1; }
-
-thread_local char g_err[512] = "";
+static thread_local char g_err[512] = "";
 
 int fail(int code, const char *fmt, ...) {
     va_list ap;
@@ -29,7 +25,15 @@ int hip_fail(const char *what, hipError_t e) {
     return fail(QTIP_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+}  // namespace qtip
+
+namespace {
+
+using qtip::aligned, qtip::fail, qtip::g_err, qtip::hip_fail;
+
+bool is_hyb(int code_id) { return code_id == QTIP_CODE_HYB || code_id == QTIP_CODE_HYB2; }
+bool is_lut(int code_id) { return code_id == QTIP_CODE_LUT; }
+bool has_table(int code_id) { return is_hyb(code_id) || is_lut(code_id) || code_id == QTIP_CODE_HYB1; }
 
 // Scratch of qtip_rht_decode_matvec_noalloc: the transformed activation between its two
 // kernels.  One copy per GPU, at an address of its own on each; the name below is only a

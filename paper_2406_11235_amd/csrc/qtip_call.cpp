@@ -14,6 +14,7 @@
 #include <Python.h>
 
 #include <stddef.h>
+#include <string.h>
 
 #include <type_traits>
 #include <utility>
@@ -22,8 +23,8 @@
 
 namespace {
 
-constexpr int MAX_ARGS = 20;
-enum Kind : char { POINTER, INTEGER, STREAM };
+constexpr int MAX_ARGS = 28;
+enum Kind : char { POINTER, INTEGER, REAL, STREAM };
 
 PyObject *g_address, *g_stream, *g_failed;         // binding.py: slow forms of an address and a stream; raise
 PyObject *g_current_device, *g_raw_stream;         // torch: current device, its current stream as an integer
@@ -64,6 +65,14 @@ bool take_integer(PyObject *o, unsigned long long &out) {
     const bool ok = as_integer(o, out);
     Py_DECREF(o);
     return ok;
+}
+
+// (the bits of a binary64)
+bool as_real(PyObject *o, unsigned long long &out) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) return false;
+    memcpy(&out, &v, sizeof(out));
+    return true;
 }
 
 bool as_pointer(PyObject *o, unsigned long long &out) {
@@ -131,6 +140,7 @@ PyObject *entry_call(PyObject *self, PyObject *const *args, size_t nargsf, PyObj
         bool ok;
         if (e->kind[i] == STREAM) ok = as_stream(given[i], value[i]);
         else if (e->kind[i] == INTEGER) ok = as_integer(given[i], value[i]);
+        else if (e->kind[i] == REAL) ok = as_real(given[i], value[i]);
         else ok = as_pointer(given[i] ? given[i] : Py_None, value[i]);
         if (!ok) return nullptr;
     }
@@ -199,15 +209,19 @@ template <class... A> struct Signature<int(A...)> {
     static constexpr int COUNT = sizeof...(A);
     template <class T> static T pass(unsigned long long v) {
         if constexpr (std::is_pointer_v<T>) return reinterpret_cast<T>(static_cast<uintptr_t>(v));
-        else return static_cast<T>(v);
+        else if constexpr (std::is_floating_point_v<T>) {
+            double d;
+            memcpy(&d, &v, sizeof(d));
+            return static_cast<T>(d);
+        } else return static_cast<T>(v);
     }
     template <size_t... I> static int call(void *f, const unsigned long long *v, std::index_sequence<I...>) {
         return reinterpret_cast<int (*)(A...)>(f)(pass<A>(v[I])...);
     }
     static int invoke(void *f, const unsigned long long *v) { return call(f, v, std::index_sequence_for<A...>{}); }
     static void kinds(Kind *kind) {
-        constexpr bool pointer[] = {std::is_pointer_v<A>...};
-        for (int i = 0; i < COUNT; i++) kind[i] = pointer[i] ? POINTER : INTEGER;
+        constexpr Kind of[] = {std::is_pointer_v<A> ? POINTER : std::is_floating_point_v<A> ? REAL : INTEGER...};
+        for (int i = 0; i < COUNT; i++) kind[i] = of[i];
     }
 };
 
@@ -286,7 +300,15 @@ PyMODINIT_FUNC PyInit__call(void) {
               "workspace", "workspace_bytes", "stream") &&
         ENTRY(qtip_block_ldl, 7, "H", "n", "g", "A_out", "D_out", "workspace", "workspace_bytes", "stream") &&
         ENTRY(qtip_quantize_ldlq, 14, "W", "A", "m", "n", "L", "k", "V", "code_id", "lut", "codes_out", "What_out",
-              "tile_err", "workspace", "workspace_bytes", "stream");
+              "tile_err", "workspace", "workspace_bytes", "stream") &&
+        ENTRY(qtip_quantize_rows_i8, 11, "x", "up", "type", "rows", "n", "ldx", "signs", "block", "q", "ldq", "scale", "stream") &&
+        ENTRY(qtip_matmul_i8, 15, "W", "ldw", "w_scale", "m", "n", "X", "ldx", "x_scale", "B", "bias", "Y", "ldy", "y_type",
+              "workspace", "workspace_bytes", "stream") &&
+        ENTRY(qtip_norm_residual, 24, "y", "ldy", "y_type", "h", "ldh", "h_type", "gate", "ldgate", "rows", "n", "norm",
+              "post_weight", "post_bias", "pre_weight", "pre_bias", "eps", "res_scale", "signs", "block", "h_out", "x", "ldx",
+              "x_type", "x_scale", "stream") &&
+        ENTRY(qtip_moe_i8, 21, "x", "ldx", "type", "T", "n", "router", "router_bias", "E", "top_k", "renormalize", "W_up",
+              "up_scale", "f", "W_down", "down_scale", "y", "ldy", "ids", "weights", "workspace", "workspace_bytes", "stream");
 #undef ENTRY
     return ok ? m : nullptr;
 }

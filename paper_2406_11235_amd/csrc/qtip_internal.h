@@ -5,6 +5,11 @@
 
 namespace qtip {
 
+// The error string of the calling thread (qtip_api.hip): both return their error code.
+int fail(int code, const char *fmt, ...);
+int hip_fail(const char *what, hipError_t e);
+inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
 constexpr int CUS = 256;  // compute units, and so workgroups in a round of one each
 
 hipError_t launch_dequantize(int k, int code_id, const uint32_t *codes, const uint32_t *lut, int m,
@@ -59,5 +64,51 @@ size_t quantize_ldlq_workspace(int m, int n, int k, int V, long tiles);
 hipError_t launch_quantize_ldlq(int k, int V, int code_id, const float *W, const float *A, int m, int n,
                                 const uint32_t *lut, uint32_t *codes, float *What, float *tile_err,
                                 void *ws, size_t ws_bytes, hipStream_t st);
+
+// QTIP_F16 and so on of the header.
+constexpr int TYPE_F16 = 0, TYPE_BF16 = 1, TYPE_F32 = 2, TYPE_I8 = 3;
+
+// Rows to 8 bits, and norms with gate and residual (qtip_rows.hip).  Null pointers: not there.
+constexpr int ROWS_MAX_N = 32768;
+hipError_t launch_quantize_rows_i8(const void *x, const void *up, int type, int rows, int n, int64_t ldx, const int8_t *signs,
+                                   int block, int8_t *q, int64_t ldq, float *scale, hipStream_t st);
+struct NormResidual {
+    const void *y, *h, *gate;
+    void *h_out, *x;
+    const float *post, *post_bias, *pre, *pre_bias;
+    const int8_t *signs;
+    float *x_scale;
+    int64_t ldy, ldh, ldgate, ldx;
+    int n, layer, x_type, p;
+    float eps, res_scale;
+};
+hipError_t launch_norm_residual(NormResidual a, int y_type, int h_type, int rows, int block, hipStream_t st);
+
+// The product of 8-bit rows with 8-bit weights (qtip_i8.hip).
+struct MatmulI8 {
+    const int8_t *W, *X;
+    const float *w_scale, *x_scale, *bias;
+    void *Y;
+    int64_t ldw, ldx, ldy;
+    int m, n, B, y_type;
+};
+size_t matmul_i8_workspace(int m, int n, int B);
+hipError_t launch_matmul_i8(const MatmulI8 &a, void *ws, hipStream_t st);
+
+// A mixture-of-experts layer for a few tokens (qtip_moe.hip).
+constexpr int MOE_MAX_TOKENS = 64, MOE_MAX_EXPERTS = 256, MOE_MAX_TOP_K = 16;
+struct MoeI8 {
+    const void *x, *router;
+    const float *router_bias;
+    const int8_t *W_up, *W_down;
+    const float *up_scale, *down_scale;
+    void *y;
+    int32_t *ids;
+    float *weights;
+    int64_t ldx, ldy;
+    int type, T, n, f, E, top_k, renormalize;
+};
+size_t moe_i8_workspace(int T, int f, int E, int top_k);
+hipError_t launch_moe_i8(const MoeI8 &a, void *ws, hipStream_t st);
 
 }  // namespace qtip

@@ -1,0 +1,229 @@
+"""qtip_moe_i8 against a plain 64-bit statement."""
+import math
+
+import pytest
+
+from layers_util import EPS, EPS32, LEAST, TYPES, Rim, generator, normal, silu
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def q():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2406_11235_amd as q
+    q.lib()
+    return q
+
+
+class Layer:
+    def __init__(self, q, T, n, f, E, top_k, dtype, seed=0, pad=0):
+        import torch
+        self.q, self.T, self.n, self.f, self.E, self.top_k, self.dtype = q, T, n, f, E, top_k, dtype
+        g = self.g = generator(seed + 11 * T + n + f + E)
+        self.x = Rim(T, n, TYPES[dtype], n + 8 * pad, 8 * pad).set(normal(g, T, n))
+        self.router = (normal(g, E, n) / math.sqrt(n)).to(TYPES[dtype])
+        self.bias = None
+        weights = lambda *shape: torch.randint(-127, 128, shape, device="cuda", generator=g, dtype=torch.int8)
+        scales = lambda *shape: 0.5 + torch.rand(*shape, device="cuda", generator=g)
+        self.W_up, self.up_scale = weights(E, 2 * f, n), scales(E, 2 * f) / (60 * math.sqrt(n))
+        self.W_down, self.down_scale = weights(E, n, f), scales(E, n) / (60 * math.sqrt(f))
+        self.y = Rim(T, n, TYPES[dtype], n + 3 * pad, pad)
+        self.ids = torch.full((T, top_k), -5, dtype=torch.int32, device="cuda")
+        self.weights = torch.full((T, top_k), -5.0, device="cuda")
+        need = q.qtip_moe_i8_workspace(T, n, f, E, top_k)
+        self.space = torch.full((need + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+        self.need = need
+
+    def call(self, renormalize=1, ids=True):
+        import torch
+        q = self.q
+        q.qtip_moe_i8(self.x.pointer, self.x.ld, q.F16 if self.dtype == "f16" else q.BF16, self.T, self.n, self.router, self.bias,
+                      self.E, self.top_k, renormalize, self.W_up, self.up_scale, self.f, self.W_down, self.down_scale,
+                      self.y.pointer, self.y.ld, self.ids if ids else None, self.weights if ids else None, self.space, self.need)
+        torch.cuda.synchronize()
+        assert self.y.rim_is_whole() and self.x.rim_is_whole() and bool((self.space[self.need:] == 0xA5).all())
+
+    def logits(self):
+        l = self.x.view.double() @ self.router.double().t().contiguous()
+        return l if self.bias is None else l + self.bias.double()
+
+    def check(self, renormalize=1):
+        """The choice may differ from the 64-bit one only between logits nearer than binary32 tells them apart; the rest is
+        checked for the choice that was made."""
+        import torch
+        l, T, E, k = self.logits(), self.T, self.E, self.top_k
+        ids, weights = self.ids.long(), self.weights.double()
+        assert int(ids.min()) >= 0 and int(ids.max()) < E
+        assert all(len(set(row)) == k for row in ids.tolist())
+        order = torch.argsort(l, dim=1, descending=True, stable=True)[:, :k]
+        # (a sum of n products in at most n / 256 + 16 roundings in line)
+        error = (self.n / 256 + 16) * EPS32 * (self.x.view.double().abs() @ self.router.double().abs().t().contiguous())
+        error = error.amax(dim=1, keepdim=True) + EPS32 * 4
+        near = (l.gather(1, ids) - l.gather(1, order)).abs()
+        near = torch.where(ids == order, torch.zeros_like(near), near)
+        assert bool((near <= 2 * error).all())
+        p = torch.exp(l - l.amax(dim=1, keepdim=True))
+        chosen = p.gather(1, ids)
+        want = chosen / (chosen.sum(dim=1, keepdim=True) if renormalize else p.sum(dim=1, keepdim=True))
+        # exp of a difference that is off by twice a logit's error, its own rounding (as its argument's), sums and a division
+        spread = (l.amax(dim=1, keepdim=True) - l.gather(1, ids)).clamp(max=100)
+        assert bool(((weights - want).abs() <= want * (4 * error + (20 + 4 * spread) * 2 * EPS32) + 1e-37).all())
+        # y, for these ids and weights
+        y, size = torch.zeros(T, self.n, dtype=torch.float64, device="cuda"), torch.zeros(T, self.n, dtype=torch.float64, device="cuda")
+        x = self.x.view.double()
+        for t in range(T):
+            for j in range(k):
+                w = float(weights[t, j])
+                if w == 0:
+                    continue
+                e = int(ids[t, j])
+                up, down = self.W_up[e].double(), self.W_down[e].double()
+                z = (up @ x[t]) * self.up_scale[e].double()
+                g, u = z[:self.f], z[self.f:]
+                h = silu(g) * u
+                # what binary32 sums of n products may be off: n / 64 + 16 roundings in line
+                bound = (self.n / 64 + 16) * EPS32 * (up.abs() @ x[t].abs()) * self.up_scale[e].double()
+                off = (bound[:self.f] * 1.1 + (8 + g.abs()) * 2 * EPS32 * silu(g).abs()) * u.abs() + bound[self.f:] * silu(g).abs()
+                off = off + 2.0 ** -17 * h.abs()  # h as two bf16 numbers
+                y[t] += w * (down @ h) * self.down_scale[e].double()
+                size[t] += w * (down.abs() @ (off + (self.f / 32 + 64) * EPS32 * h.abs())) * self.down_scale[e].double()
+        off = (self.y.view.double() - y).abs()
+        assert bool((off <= size + EPS[self.dtype] * (y.abs() + size) + LEAST[self.dtype]).all()), float((off - size).max())
+
+
+SHAPES = [(1, 16, 16, 1, 1), (1, 64, 32, 4, 2), (2, 48, 80, 3, 3), (3, 272, 144, 7, 2), (1, 1024, 512, 8, 2), (4, 512, 256, 64, 8),
+          (7, 1040, 400, 65, 6), (16, 256, 128, 16, 4), (17, 512, 272, 5, 5), (32, 256, 256, 128, 8), (33, 640, 112, 200, 16),
+          (64, 512, 256, 256, 8), (64, 128, 64, 2, 1), (50, 96, 48, 1, 1), (5, 4096, 1024, 3, 1)]
+
+
+@pytest.mark.parametrize("T,n,f,E,top_k", SHAPES)
+@pytest.mark.parametrize("dtype,renormalize,pad", [("f16", 1, 0), ("bf16", 0, 1)])
+def test_against_64_bits(q, T, n, f, E, top_k, dtype, renormalize, pad):
+    layer = Layer(q, T, n, f, E, top_k, dtype, pad=pad)
+    layer.call(renormalize)
+    layer.check(renormalize)
+
+
+def test_all_tokens_to_one_expert_and_one_token_each(q):
+    import torch
+    layer = Layer(q, 64, 256, 128, 64, 1, "bf16")
+    layer.bias = torch.zeros(64, device="cuda")
+    layer.bias[17] = 100.0
+    layer.call()
+    assert bool((layer.ids == 17).all())
+    layer.check()
+    # x one-hot and a router that sends token t to expert t
+    layer = Layer(q, 64, 256, 128, 64, 1, "bf16")
+    layer.x.view.zero_()
+    layer.x.view[torch.arange(64), torch.arange(64)] = 1.0
+    layer.router.zero_()
+    layer.router[torch.arange(64), torch.arange(64)] = 5.0
+    layer.call()
+    assert layer.ids[:, 0].tolist() == list(range(64))
+    layer.check()
+
+
+def test_ties_go_to_the_lowest_expert(q):
+    import torch
+    for E in (8, 64, 130, 256):
+        layer = Layer(q, 5, 64, 32, E, 4 if E == 8 else 8, "f16")
+        layer.router.zero_()
+        layer.call(0)
+        assert layer.ids.tolist() == [list(range(layer.top_k))] * 5
+        assert bool(((layer.weights.double() - 1 / E).abs() <= 20 * EPS32 / E).all())
+        layer.bias = torch.zeros(E, device="cuda")
+        layer.bias[E - 1], layer.bias[3] = 1.0, 1.0
+        layer.call()
+        assert layer.ids.tolist() == [[3, E - 1] + [e for e in range(E) if e not in (3, E - 1)][:layer.top_k - 2]] * 5
+        layer.check()
+
+
+def test_masked_experts(q):
+    import torch
+    inf = float("inf")
+    layer = Layer(q, 6, 128, 64, 10, 4, "bf16")
+    layer.bias = torch.full((10,), -inf, device="cuda")
+    layer.bias[2], layer.bias[7] = 0.0, 0.5
+    layer.call()
+    assert bool((layer.weights[:, 2:] == 0).all())
+    assert bool((layer.ids[:, :2].sort(dim=1).values == torch.tensor([2, 7], device="cuda")).all())
+    layer.check()
+    # the lowest finite values mask too: their exponentials are nothing
+    layer.bias[layer.bias == -inf] = torch.finfo(torch.float32).min
+    layer.call()
+    assert bool((layer.weights[:, 2:] == 0).all())
+    # no expert at all: nothing comes out
+    layer.bias.fill_(-inf)
+    layer.y.view.fill_(3.0)
+    layer.call()
+    assert bool((layer.weights == 0).all()) and bool((layer.y.view == 0).all())
+    assert int(layer.ids.min()) >= 0 and int(layer.ids.max()) < 10
+
+
+def test_a_token_that_is_not_finite_is_alone_in_it(q):
+    import torch
+    for bad in (float("nan"), float("inf")):
+        layer = Layer(q, 20, 256, 128, 12, 3, "f16")
+        layer.call()
+        y, ids, weights = layer.y.view.clone(), layer.ids.clone(), layer.weights.clone()
+        layer.x.view[4, 9], layer.x.view[19, 255] = bad, bad
+        layer.call()
+        assert int(layer.ids.min()) >= 0 and int(layer.ids.max()) < 12
+        for t in range(20):
+            if t in (4, 19):
+                assert bool(torch.isnan(layer.weights[t]).all()) and bool(torch.isnan(layer.y.view[t]).all())
+            else:
+                assert torch.equal(layer.y.view[t], y[t]) and torch.equal(layer.ids[t], ids[t])
+                assert torch.equal(layer.weights[t], weights[t])
+
+
+def test_large_values_of_h(q):
+    """silu(g) .* u beyond fp16's range inside, a result within it."""
+    layer = Layer(q, 3, 256, 128, 4, 2, "f16")
+    layer.up_scale *= 2000
+    layer.down_scale *= 1e-6
+    layer.call()
+    layer.check()
+
+
+def test_without_ids_and_twice_the_same(q):
+    import torch
+    layer = Layer(q, 23, 512, 256, 40, 5, "bf16")
+    layer.call()
+    y = layer.y.view.clone()
+    layer.space.fill_(0x5A)
+    layer.space[layer.need:] = 0xA5
+    layer.call(ids=False)
+    assert torch.equal(layer.y.view, y)
+
+
+def test_replayed_from_a_graph(q):
+    import torch
+    layer = Layer(q, 9, 512, 256, 24, 4, "bf16")
+    side = torch.cuda.Stream()
+
+    def enqueue():
+        q.qtip_moe_i8(layer.x.pointer, layer.x.ld, q.BF16, 9, 512, layer.router, None, 24, 4, 1, layer.W_up, layer.up_scale, 256,
+                      layer.W_down, layer.down_scale, layer.y.pointer, layer.y.ld, layer.ids, layer.weights, layer.space, layer.need)
+
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        enqueue()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        enqueue()
+    for replay in range(3):
+        layer.x.view.copy_(normal(layer.g, 9, 512))
+        layer.call()
+        want = layer.y.view.clone(), layer.ids.clone()
+        layer.y.view.zero_()
+        layer.ids.zero_()
+        layer.space.fill_(0xA5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(layer.y.view, want[0]) and torch.equal(layer.ids, want[1]), replay
