@@ -310,6 +310,7 @@ int qtip_quantize_ldlq(const float *W, const float *A, int m, int n, int L, int 
 
 #define QTIP_ROWS_MAX_N 32768 /* longest row of the calls that hold one in registers */
 #define QTIP_I8_MAX_N 131071  /* most inputs of an 8-bit product: n 128^2 stays below 2^31 */
+#define QTIP_I8_MAX_LD (1 << 24) /* most values between two rows of an 8-bit product's operands */
 #define QTIP_I8_MAX_B (65535 * 16)
 
 /*

@@ -12,7 +12,7 @@ CALL = os.path.join(HERE, "_call" + (sysconfig.get_config_var("EXT_SUFFIX") or "
 CALL_SOURCE = os.path.join(CSRC, "qtip_call.cpp")
 SOURCES = ["qtip_api.hip", "qtip_decode.hip", "qtip_lut14.hip", "qtip_gemm.hip", "qtip_rht.hip", "qtip_viterbi.hip", "qtip_ldlq.hip", "qtip_quantize.cpp",
            "qtip_api_i8.hip", "qtip_rows.hip", "qtip_i8.hip", "qtip_moe.hip"]
-HEADERS = ["qtip_device.h", "qtip_rht_device.h", "qtip_rows_device.h", "qtip_internal.h", os.path.join("..", "..", "include", "qtip.h")]
+HEADERS = ["qtip_device.h", "qtip_rht_device.h", "qtip_rows_device.h", "qtip_copy_device.h", "qtip_internal.h", os.path.join("..", "..", "include", "qtip.h")]
 
 # Packed-FP32 VALU forms are switched off for every device compile.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-pthread",

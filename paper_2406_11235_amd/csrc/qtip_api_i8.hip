@@ -71,6 +71,8 @@ int qtip_matmul_i8(const int8_t *W, int64_t ldw, const float *w_scale, int m, in
     if (int rc = check_matrix(fn, "Y", Y, ldy, m, y_type)) return rc;
     if (ldw % 16 || ldx % 16 || !aligned(W, 16) || !aligned(X, 16))
         return fail(QTIP_EINVAL, "%s: rows of W and X must begin at multiples of 16 bytes", fn);
+    if (ldw > QTIP_I8_MAX_LD || ldx > QTIP_I8_MAX_LD)
+        return fail(QTIP_EINVAL, "%s: rows of W or X are more than QTIP_I8_MAX_LD = %d values apart", fn, QTIP_I8_MAX_LD);
     if (!aligned(w_scale, 4) || !aligned(x_scale, 4) || !aligned(bias, 4))
         return fail(QTIP_EINVAL, "%s: scales and bias must be 4-byte aligned", fn);
     const size_t need = qtip::matmul_i8_workspace(m, n, B);

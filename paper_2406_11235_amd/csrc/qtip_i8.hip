@@ -1,6 +1,8 @@
 // The product of 8-bit rows with 8-bit weights: Y[b][i] = w_scale[i] x_scale[b] sum_j W[i][j] X[b][j] + bias[i], the sum
 // exact in 32-bit whole numbers.
-#include "qtip_device.h"
+#include <type_traits>
+
+#include "qtip_copy_device.h"
 #include "qtip_internal.h"
 #include "qtip_rows_device.h"
 
@@ -10,16 +12,14 @@ namespace {
 
 typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
 
-// 16 bytes at position k of a row of n; what stands behind the row's end is taken as zeros.
-__device__ __forceinline__ i32x4_t load_units(const int8_t *row, int k, int n) {
-    i32x4_t v = {0, 0, 0, 0};
-    if (k < n) v = *reinterpret_cast<const i32x4_t *>(row + k);
-    if (k + 16 > n) {
+constexpr int FEW_ROWS = 32;  // batch rows that are taken at once, weights read once
+
+// The first `count` of 16 bytes, zeros behind them.
+__device__ __forceinline__ i32x4_t keep_bytes(i32x4_t v, int count) {
 #pragma unroll
-        for (int d = 0; d < 4; d++) {
-            const int left = n - k - 4 * d;  // bytes of this word that belong to the row
-            if (left < 4) v[d] = left <= 0 ? 0 : v[d] & (int)(0xFFFFFFFFu >> (32 - 8 * left));
-        }
+    for (int d = 0; d < 4; d++) {
+        const int left = count - 4 * d;
+        if (left < 4) v[d] = left <= 0 ? 0 : v[d] & (int)(0xFFFFFFFFu >> (32 - 8 * left));
     }
     return v;
 }
@@ -27,51 +27,348 @@ __device__ __forceinline__ i32x4_t load_units(const int8_t *row, int k, int n) {
 // Four neighbouring outputs of batch row b.
 template <class T>
 __device__ __forceinline__ void store_outputs(const MatmulI8 &a, int b, int i, i32x4_t sum) {
-    const float xs = a.x_scale[b];
-    float4_t v;
-#pragma unroll
-    for (int r = 0; r < 4; r++) {
-        const int at = min(i + r, a.m - 1);
-        v[r] = (float)sum[r] * (a.w_scale[at] * xs) + (a.bias ? a.bias[at] : 0.f);
-    }
+    const float4_t scale = load_quad(a.w_scale, i, a.m) * a.x_scale[b];
+    float4_t v = __builtin_convertvector(sum, float4_t) * scale;
+    if (a.bias) v += load_quad(a.bias, i, a.m);
     store_quad((T *)a.Y + (int64_t)b * a.ldy, i, a.m, v);
 }
 
-// 16 outputs x 16 batch rows by a workgroup; its waves take 128 inputs in turn.
-template <class T, int NW> __global__ __launch_bounds__(NW * 64) void matmul_i8_few_kernel(MatmulI8 a) {
-    __shared__ i32x4_t s_sum[NW][64];
+// 16 MR outputs x 8 XC batch rows by a workgroup; its waves take 128 inputs in turn and add up at the end.  Each wave has a
+// ring of D stages in LDS to itself, filled by copies past the registers, eight whole rows of 128 bytes each: so many
+// bytes can be under way at a time, and no wave waits for another before the end.  Unit c (16 bytes) of row r is at place
+// c ^ (r / 2 % 8): 16 rows one after the other have the same unit in different banks.
+template <class T, int MR, int XC, int NW, int D>
+__global__ __launch_bounds__(NW * 64) void matmul_i8_few_kernel(MatmulI8 a) {
+    constexpr int NB = (XC + 1) / 2, WC = 2 * MR, STAGE = (WC + 2 * NB) * 1024;
+    constexpr int LDS = NW * D * STAGE > NW * MR * NB * 1024 ? NW * D * STAGE : NW * MR * NB * 1024;
+    __shared__ __attribute__((aligned(1024))) char s_ring[LDS];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int i0 = blockIdx.x * 16, b0 = blockIdx.y * 16;
-    const int8_t *w = a.W + (int64_t)min(i0 + (lane & 15), a.m - 1) * a.ldw;
-    const int8_t *x = a.X + (int64_t)min(b0 + (lane & 15), a.B - 1) * a.ldx;
-    i32x4_t sum = {0, 0, 0, 0};
-    for (int c = wave * 128; c < a.n; c += NW * 128) {
-        const int k = c + 32 * (lane >> 4);
-        // (weights behind the row's end meet zeros of x)
-        const i32x4_t w0 = load_units(w, k, a.n), w1 = load_units(w, k + 16, a.n);
-        const i32x4_t x0 = load_units(x, k, a.n), x1 = load_units(x, k + 16, a.n);
-        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(w0, x0, sum, 0, 0, 0);
-        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(w1, x1, sum, 0, 0, 0);
-    }
-    s_sum[wave][lane] = sum;
-    __syncthreads();
-    if (wave != 0) return;
+    const int i0 = blockIdx.x * 16 * MR, b0 = blockIdx.y * 8 * XC;
+    const int rows_w = min(16 * MR, a.m - i0), rows_x = min(8 * XC, a.B - b0), ends = (a.n + 15) & ~15;
+    const u32x4_t buffer_w = buffer_of(a.W + (int64_t)i0 * a.ldw, (size_t)(rows_w - 1) * a.ldw + ends);
+    const u32x4_t buffer_x = buffer_of(a.X + (int64_t)b0 * a.ldx, (size_t)(rows_x - 1) * a.ldx + ends);
+    char *const ring = s_ring + wave * D * STAGE;
+    // (rows behind the last are the last once more)
+    uint32_t at_w[WC], at_x[XC];
+    int unit[2];  // of even and of odd copies
 #pragma unroll
-    for (int other = 1; other < NW; other++) sum += s_sum[other][lane];
-    const int b = b0 + (lane & 15), i = i0 + 4 * (lane >> 4);
-    if (b < a.B && i < a.m) store_outputs<T>(a, b, i, sum);
+    for (int o = 0; o < 2; o++) unit[o] = 16 * ((lane & 7) ^ (4 * o + (lane >> 4)));
+#pragma unroll
+    for (int g = 0; g < WC; g++) at_w[g] = (uint32_t)min(8 * g + (lane >> 3), rows_w - 1) * (uint32_t)a.ldw + unit[g & 1];
+#pragma unroll
+    for (int g = 0; g < XC; g++) at_x[g] = (uint32_t)min(8 * g + (lane >> 3), rows_x - 1) * (uint32_t)a.ldx + unit[g & 1];
+    const int stages = (a.n + 127) / 128;
+    auto copy = [&](int s, int slot) {
+        const uint32_t k = s * 128;
+#pragma unroll
+        for (int g = 0; g < WC; g++) copy_to_lds(buffer_w, at_w[g], k, ring + slot * STAGE + g * 1024);
+        // (behind a row's end: zeros for X, whatever the weights have there)
+#pragma unroll
+        for (int g = 0; g < XC; g++)
+            copy_to_lds(buffer_x, (int)k + unit[g & 1] >= a.n ? 0xFFFFFF00u : at_x[g], k, ring + slot * STAGE + (WC + g) * 1024);
+    };
+    i32x4_t sum[MR][NB];
+#pragma unroll
+    for (int r = 0; r < MR; r++)
+#pragma unroll
+        for (int c = 0; c < NB; c++) sum[r][c] = i32x4_t{0, 0, 0, 0};
+    const int row = (lane & 15) * 128, turn = lane >> 1 & 7, hi = lane >> 4;
+    auto products = [&](int s, int slot, auto again) {
+        char *const stage = ring + slot * STAGE;
+        const int left = a.n - s * 128;
+        if (left < 128 && (left & 15)) {  // what X's last unit has behind the row's end
+            if (lane < 16 * NB) {
+                i32x4_t *p = reinterpret_cast<i32x4_t *>(stage + WC * 1024 + lane * 128 + (((left >> 4) ^ (lane >> 1 & 7)) << 4));
+                *p = keep_bytes(*p, left & 15);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+        i32x4_t w[MR][2], x[NB][2];
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const char *p = stage + row + (((4 * h + hi) ^ turn) << 4);
+#pragma unroll
+            for (int r = 0; r < MR; r++) w[r][h] = *reinterpret_cast<const i32x4_t *>(p + r * 2048);
+#pragma unroll
+            for (int c = 0; c < NB; c++) x[c][h] = *reinterpret_cast<const i32x4_t *>(p + WC * 1024 + c * 2048);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        again();
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int r = 0; r < MR; r++)
+#pragma unroll
+                for (int c = 0; c < NB; c++) sum[r][c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[r][h], x[c][h], sum[r][c], 0, 0, 0);
+    };
+    const int mine = (stages - wave + NW - 1) / NW;  // stages wave, wave + NW, ...
+#pragma unroll
+    for (int d = 0; d < D; d++)
+        if (d < mine) copy(wave + d * NW, d);
+    int j = 0;
+    for (; j + D < mine; j++) {
+        __builtin_amdgcn_s_waitcnt(vmcnt_only((D - 1) * (WC + XC)));
+        asm volatile("" ::: "memory");
+        products(wave + j * NW, j % D, [&] { copy(wave + (j + D) * NW, j % D); });
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+    asm volatile("" ::: "memory");
+    for (; j < mine; j++) products(wave + j * NW, j % D, [] {});
+    __syncthreads();
+    auto *const sums = reinterpret_cast<i32x4_t(*)[MR * NB][64]>(s_ring);
+#pragma unroll
+    for (int r = 0; r < MR; r++)
+#pragma unroll
+        for (int c = 0; c < NB; c++) sums[wave][r * NB + c][lane] = sum[r][c];
+    __syncthreads();
+    for (int o = wave; o < MR * NB; o += NW) {
+        i32x4_t t = sums[0][o][lane];
+#pragma unroll
+        for (int other = 1; other < NW; other++) t += sums[other][o][lane];
+        const int b = o % NB * 16 + (lane & 15), i = i0 + o / NB * 16 + 4 * (lane >> 4);
+        if (b < rows_x && i < a.m) store_outputs<T>(a, b0 + b, i, t);
+    }
+}
+
+// A stage of the tiled product is 128 inputs of a tile's rows: 128 bytes a row in LDS, eight units of 16 bytes, unit c of
+// row r at place c ^ (r / 2 % 8), so that 16 rows one after the other have the same unit in different places of two rows' 256
+// bytes, the width of the banks.
+constexpr int STAGE_K = 128;
+
+// BM outputs x BN batch rows by a workgroup of WM x WN waves, RA x RB blocks of 16 x 16 each: weights are the rows of the matrix
+// instruction's result, batch rows its columns.  Both come into LDS by copies past the registers, a stage ahead.
+template <class T, int WM, int WN, int RA, int RB, int RING>
+__global__ __launch_bounds__(WM *WN * 64) void matmul_i8_tile_kernel(MatmulI8 a, int tiles_m, int tiles_b, int parts, int32_t *sums) {
+    constexpr int NW = WM * WN, BM = 16 * RA * WM, BN = 16 * RB * WN, STAGE = (BM + BN) * STAGE_K;
+    constexpr int GA = BM / 8 / NW, GB = BN / 8 / NW;  // copies of a wave and stage: 8 rows each
+    static_assert(GA * NW * 8 == BM && GB * NW * 8 == BN, "whole copies");
+    constexpr int READS = RA + RB > 8 ? 3 : 8;  // operands read between a row of blocks and the next
+    __shared__ __attribute__((aligned(1024))) char s_tile[RING * STAGE];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+
+    // Workgroups go round the eight XCDs: each XCD takes a run of tiles, four batch tiles at a time for all outputs, so
+    // that those it has at one time share rows of both sides in its L2.
+    const int tiles = tiles_m * tiles_b, per = (tiles * parts + 7) / 8;
+    const int number = (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
+    if (number >= tiles * parts || (int)(blockIdx.x / 8) >= per) return;
+    const int part = number / tiles, t = number - part * tiles;
+    constexpr int GROUP = 4;
+    const int group = t / (GROUP * tiles_m), in_group = t - group * GROUP * tiles_m;
+    const int wide = min(GROUP, tiles_b - group * GROUP);
+    const int i0 = in_group / wide * BM, b0 = (group * GROUP + in_group % wide) * BN;
+
+    const int rows_a = min(BM, a.m - i0), rows_b = min(BN, a.B - b0), ends = (a.n + 15) & ~15;
+    const u32x4_t buffer_a = buffer_of(a.W + (int64_t)i0 * a.ldw, (size_t)(rows_a - 1) * a.ldw + ends);
+    const u32x4_t buffer_b = buffer_of(a.X + (int64_t)b0 * a.ldx, (size_t)(rows_b - 1) * a.ldx + ends);
+    // (rows behind the last are the last once more)
+    static_assert(NW % 2 == 0, "a wave's copies are all of even or all of odd groups of 8 rows");
+    const int unit = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
+    uint32_t at_a[GA], at_b[GB];
+#pragma unroll
+    for (int g = 0; g < GA; g++) at_a[g] = (uint32_t)min((g * NW + wave) * 8 + (lane >> 3), rows_a - 1) * (uint32_t)a.ldw + unit * 16;
+#pragma unroll
+    for (int g = 0; g < GB; g++) at_b[g] = (uint32_t)min((g * NW + wave) * 8 + (lane >> 3), rows_b - 1) * (uint32_t)a.ldx + unit * 16;
+    // this part's stages: from `begin` on, up to `stages`
+    const int all = (a.n + STAGE_K - 1) / STAGE_K, begin = (int)((int64_t)all * part / parts), stages = (int)((int64_t)all * (part + 1) / parts);
+    // the copy number g of stage s into place `slot` of the ring
+    auto copy = [&](int s, int slot, int g) {
+        char *to = s_tile + slot * STAGE + wave * 1024;
+        const uint32_t k = s * STAGE_K;
+        // (behind a row's end: zeros for X, whatever the weights have there)
+        if (g < GA) copy_to_lds(buffer_a, at_a[g], k, to + g * NW * 1024);
+        else copy_to_lds(buffer_b, (int)k + unit * 16 >= a.n ? 0xFFFFFF00u : at_b[g - GA], k, to + BM * STAGE_K + (g - GA) * NW * 1024);
+    };
+
+    const int wm = wave % WM, wn = wave / WM;
+    const int base = (lane & 15) * STAGE_K, r8 = (lane >> 1) & 7, hi = lane >> 4;
+    i32x4_t fa[2][RA], fb[2][RB];
+    // operand number o of half kk of the stage in `slot`: RA of weights, then RB of X
+    auto fetch = [&](int slot, int kk, int o) {
+        const char *p = s_tile + slot * STAGE + base + (((kk * 4 + hi) ^ r8) << 4);
+        if (o < RA) fa[kk][o] = *reinterpret_cast<const i32x4_t *>(p + (wm * RA + o) * 16 * STAGE_K);
+        else fb[kk][o - RA] = *reinterpret_cast<const i32x4_t *>(p + (BM + (wn * RB + o - RA) * 16) * STAGE_K);
+    };
+    i32x4_t sum[RA][RB];
+#pragma unroll
+    for (int r = 0; r < RA; r++)
+#pragma unroll
+        for (int c = 0; c < RB; c++) sum[r][c] = i32x4_t{0, 0, 0, 0};
+
+    // What a row's last unit has behind its end, in the last stage of X.
+    auto mask = [&](int s, int slot) {
+        const int left = a.n - s * STAGE_K;
+        if (left >= STAGE_K || (left & 15) == 0) return;
+        for (int r = threadIdx.x; r < BN; r += NW * 64) {
+            i32x4_t *p = reinterpret_cast<i32x4_t *>(s_tile + slot * STAGE + (BM + r) * STAGE_K + (((left >> 4) ^ (r >> 1 & 7)) << 4));
+            *p = keep_bytes(*p, left & 15);
+        }
+        __syncthreads();
+    };
+    // everyone's copies up to stage s are there (at most `most` stages behind it may be under way), and nobody reads stage s - 1
+    // any more
+    auto meet = [&](int s, int slot, int most) {
+        static_assert(RING <= 3, "at most two stages behind");
+        const int behind = min(stages - 1 - s, most);
+        if (behind == 0) __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+        else if (behind == 1) __builtin_amdgcn_s_waitcnt(vmcnt_only(GA + GB));
+        else __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * (GA + GB)));
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        mask(s, slot);
+    };
+
+#pragma unroll
+    for (int d = 0; d < RING; d++)
+        if (begin + d < stages) {
+#pragma unroll
+            for (int g = 0; g < GA + GB; g++) copy(begin + d, d, g);
+        }
+    meet(begin, 0, RING - 1);
+#pragma unroll
+    for (int o = 0; o < RA + RB; o++) fetch(0, 0, o);
+    // One half of a stage: the products of its operands, and between them the operands of the next half (of the stage at `next`)
+    // and, in the second half, copies: issued at once they would keep the matrix cores waiting.
+    auto half = [&](auto kk, int next, bool read, int copied, int slot, bool more) {
+#pragma unroll
+        for (int r = 0; r < RA; r++) {
+#pragma unroll
+            for (int c = 0; c < RB; c++)
+                sum[r][c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[kk][r], fb[kk][c], sum[r][c], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (read) {
+#pragma unroll
+                for (int o = r * READS; o < (r + 1) * READS && o < RA + RB; o++) fetch(next, 1 - kk, o);
+            }
+            if (more) {
+#pragma unroll
+                for (int g = r * (GA + GB) / RA; g < (r + 1) * (GA + GB) / RA; g++) copy(copied, slot, g);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    int slot = 0;
+    for (int s = begin; s < stages; s++) {
+        const int next = slot + 1 == RING ? 0 : slot + 1;
+        half(std::integral_constant<int, 0>{}, slot, true, 0, 0, false);
+        if (s + 1 < stages) meet(s + 1, next, RING - 2);
+        half(std::integral_constant<int, 1>{}, next, s + 1 < stages, s + RING, slot, s + RING < stages);
+        slot = next;
+    }
+#pragma unroll
+    for (int c = 0; c < RB; c++) {
+        const int b = b0 + (wn * RB + c) * 16 + (lane & 15);
+        if (b >= a.B) continue;
+#pragma unroll
+        for (int r = 0; r < RA; r++) {
+            const int i = i0 + (wm * RA + r) * 16 + 4 * hi;
+            if (i >= a.m) continue;
+            if (sums) *reinterpret_cast<i32x4_t *>(sums + ((int64_t)part * a.B + b) * ((a.m + 3) & ~3) + i) = sum[r][c];
+            else store_outputs<T>(a, b, i, sum[r][c]);
+        }
+    }
+}
+
+// The parts' sums.
+template <class T> __global__ __launch_bounds__(256) void matmul_i8_join_kernel(MatmulI8 a, int parts, const int32_t *__restrict__ sums) {
+    const int i = 4 * (blockIdx.x * 256 + threadIdx.x), b = blockIdx.y;
+    if (i >= a.m) return;
+    const int64_t wide = (a.m + 3) & ~3;
+    i32x4_t t = {0, 0, 0, 0};
+    for (int p = 0; p < parts; p++) t += *reinterpret_cast<const i32x4_t *>(sums + ((int64_t)p * a.B + b) * wide + i);
+    store_outputs<T>(a, b, i, t);
+}
+
+// How the product of more than 32 rows is cut: the tile, how many stages of it LDS holds, and into how many parts the
+// inputs are. Where tiles leave CUs idle, a smaller tile or parts in the inputs fill them.
+struct Cut {
+    int tile, parts;
+};
+// What a stage takes (us) while a CU has one workgroup and while it has two, with enough tiles for that on all CUs:
+// 256 x 256 with two stages in LDS, 128 x 128 with two (two workgroups on a CU) and with three (one), 128 x 64 with three.
+// Measured: 8192 x 28672, 4096 rows 736 us with 256 x 256; 8192 x 8192: 1024 rows 68.8 with 128 x 128 and two stages (94.9 with
+// 256 x 256), 512 rows 41.9 with three stages (51.7 with two), 256 rows 30.0 with 128 x 64 (37.5); 14336 x 4096: 997 rows 62.1
+// with 256 x 256 (69.9 with 128 x 128), 512 rows 37.2 with 128 x 128, 256 rows 24.9 with it (26.0 with 128 x 64).
+constexpr int TILE_M[4] = {256, 128, 128, 128}, TILE_B[4] = {256, 128, 128, 64};
+constexpr float STAGE_ONE[4] = {1.64f, 0.8f, 0.65f, 0.465f}, STAGE_TWO[4] = {3.28f, 1.08f, 1.3f, 0.73f};
+
+int64_t tiles_of(int tile, int m, int B) {
+    return ((int64_t)m + TILE_M[tile] - 1) / TILE_M[tile] * ((B + TILE_B[tile] - 1) / TILE_B[tile]);
+}
+Cut cut_of(int m, int n, int B) {
+    Cut best = {0, 1};
+    float least = 0.f;
+    const int stages = (n + STAGE_K - 1) / STAGE_K;
+    for (int tile = 0; tile < 4; tile++) {
+        const int64_t tiles = tiles_of(tile, m, B);
+        for (int parts = 1; parts <= 16; parts++) {
+            // (parts pay while they find idle CUs; a part has four stages at least)
+            if (parts > 1 && (tiles * parts > CUS || stages < 4 * parts)) break;
+            const int64_t work = tiles * parts, rest = work % (2 * CUS);
+            float cost = (float)(work / (2 * CUS)) * STAGE_TWO[tile] + (rest == 0 ? 0.f : rest <= CUS ? STAGE_ONE[tile] : STAGE_TWO[tile]);
+            cost *= (float)((stages + parts - 1) / parts);
+            // a launch, and the sums written and read: 8192 x 8192, 128 rows, 25.7 us in one part, 20.1 in two
+            if (parts > 1) cost += 2.5f + 1.6e-6f * (float)parts * (float)m * (float)B;
+            if (least == 0.f || cost < least) {
+                least = cost;
+                best = {tile, parts};
+            }
+        }
+    }
+    return best;
+}
+
+template <class T, int MR, int XC, int NW, int D> hipError_t launch_few(const MatmulI8 &a, hipStream_t st) {
+    hipLaunchKernelGGL((matmul_i8_few_kernel<T, MR, XC, NW, D>), dim3((a.m + 16 * MR - 1) / (16 * MR)), dim3(NW * 64), 0, st, a);
+    return hipGetLastError();
+}
+// Up to 32 rows: each weight is read once and all rows at once, and what counts is how many bytes are under way.  Many outputs:
+// several 16s of them a workgroup share the copies of X; few: one, with as many waves as there are stages for.
+// (us; 2 x 16 outputs, 1 x 16 by 16 waves, by 8: 8192 x 28672, 16 rows, 43.5, 46.6, 47.3; 28672 x 4096, 1 row, 25.8, 27.2, 24.8;
+// 4096 x 4096, 1 row, 5.3, 4.8, 5.8; 4096 x 28672, 16 rows, 32.1, 24.5, 25.1; 28672 x 1024, 8 rows, 9.9, 13.1, 8.5.  4 x 16 and 1 x 16
+// outputs, 32 rows: 14336 x 4096 11.5 and 19.8, 8192 x 8192 15.8 and 18.0, 4096 x 14336 17.7 and 12.0.)
+template <class T, int XC> hipError_t launch_few_rows(const MatmulI8 &a, hipStream_t st) {
+    if constexpr (XC == 4) {
+        if (a.m >= 8192) return launch_few<T, 4, XC, 8, 1>(a, st);
+        return launch_few<T, 1, XC, 8, 2>(a, st);
+    } else {
+        if (a.m >= 8192 && a.n >= 2048) return launch_few<T, 2, XC, 8, 3>(a, st);
+        if (a.n >= 4096 && a.m < 8192) return launch_few<T, 1, XC, 16, 2>(a, st);
+        return launch_few<T, 1, XC, 8, 2>(a, st);
+    }
+}
+template <class T, int TILE, int WM, int WN, int RA, int RB, int RING>
+hipError_t launch_tiles(const MatmulI8 &a, int parts, int32_t *sums, hipStream_t st) {
+    static_assert(16 * RA * WM == TILE_M[TILE] && 16 * RB * WN == TILE_B[TILE], "the tile that was chosen");
+    const int64_t work = tiles_of(TILE, a.m, a.B) * parts;
+    if (work > (1 << 30)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((matmul_i8_tile_kernel<T, WM, WN, RA, RB, RING>), dim3((uint32_t)(work + 7) / 8 * 8), dim3(WM * WN * 64), 0, st, a,
+                       (a.m + TILE_M[TILE] - 1) / TILE_M[TILE], (a.B + TILE_B[TILE] - 1) / TILE_B[TILE], parts, parts > 1 ? sums : nullptr);
+    if (parts > 1)
+        hipLaunchKernelGGL((matmul_i8_join_kernel<T>), dim3((a.m + 1023) / 1024, a.B), dim3(256), 0, st, a, parts, sums);
+    return hipGetLastError();
+}
+template <class T> hipError_t launch(const MatmulI8 &a, int32_t *sums, hipStream_t st) {
+    if (a.B <= 8) return launch_few_rows<T, 1>(a, st);
+    if (a.B <= 16) return launch_few_rows<T, 2>(a, st);
+    if (a.B <= FEW_ROWS) return launch_few_rows<T, 4>(a, st);
+    const Cut cut = cut_of(a.m, a.n, a.B);
+    if (cut.tile == 0) return launch_tiles<T, 0, 2, 4, 8, 4, 2>(a, cut.parts, sums, st);
+    if (cut.tile == 1) return launch_tiles<T, 1, 4, 2, 2, 4, 2>(a, cut.parts, sums, st);
+    if (cut.tile == 2) return launch_tiles<T, 2, 4, 2, 2, 4, 3>(a, cut.parts, sums, st);
+    return launch_tiles<T, 3, 4, 2, 2, 2, 3>(a, cut.parts, sums, st);
 }
 
 }  // namespace
 
-size_t matmul_i8_workspace(int, int, int) { return 0; }
+size_t matmul_i8_workspace(int m, int n, int B) {
+    if (B <= FEW_ROWS) return 0;
+    const Cut cut = cut_of(m, n, B);
+    return cut.parts > 1 ? (size_t)cut.parts * B * (((size_t)m + 3) & ~(size_t)3) * 4 : 0;
+}
 
-hipError_t launch_matmul_i8(const MatmulI8 &a, void *, hipStream_t st) {
-    const dim3 grid((a.m + 15) / 16, (a.B + 15) / 16);
-    if (a.y_type == TYPE_F32) hipLaunchKernelGGL((matmul_i8_few_kernel<float, 4>), grid, dim3(256), 0, st, a);
-    else if (a.y_type == TYPE_F16) hipLaunchKernelGGL((matmul_i8_few_kernel<half_t, 4>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((matmul_i8_few_kernel<bf16_t, 4>), grid, dim3(256), 0, st, a);
-    return hipGetLastError();
+hipError_t launch_matmul_i8(const MatmulI8 &a, void *ws, hipStream_t st) {
+    if (a.y_type == TYPE_F32) return launch<float>(a, (int32_t *)ws, st);
+    if (a.y_type == TYPE_F16) return launch<half_t>(a, (int32_t *)ws, st);
+    return launch<bf16_t>(a, (int32_t *)ws, st);
 }
 
 }  // namespace qtip

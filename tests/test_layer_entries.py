@@ -45,7 +45,7 @@ def test_quantize_rows_refuses(code, change):
 @pytest.mark.parametrize("code,change", [
     (EINVAL, dict(W=None)), (EINVAL, dict(X=None)), (EINVAL, dict(Y=None)), (EINVAL, dict(w_scale=None)), (EINVAL, dict(x_scale=None)),
     (EUNSUPPORTED, dict(y_type=q.I8)), (EINVAL, dict(m=0)), (EINVAL, dict(n=0)), (EINVAL, dict(B=0)), (EINVAL, dict(B=-1)),
-    (EINVAL, dict(n=131072, ldw=131072, ldx=131072)), (EINVAL, dict(B=65535 * 16 + 1)), (EINVAL, dict(ldw=48)), (EINVAL, dict(ldx=48)),
+    (EINVAL, dict(n=131072, ldw=131072, ldx=131072)), (EINVAL, dict(B=65535 * 16 + 1)), (EINVAL, dict(ldw=(1 << 24) + 16)), (EINVAL, dict(ldx=(1 << 24) + 16)), (EINVAL, dict(ldw=48)), (EINVAL, dict(ldx=48)),
     (EINVAL, dict(ldy=4)), (EINVAL, dict(ldw=72)), (EINVAL, dict(ldx=56)), (EINVAL, dict(W=P + 8)), (EINVAL, dict(X=P + 1)),
     (EINVAL, dict(Y=P + 2)), (EINVAL, dict(bias=P + 2)), (EINVAL, dict(w_scale=P + 1)), (EINVAL, dict(x_scale=P + 3))])
 def test_matmul_refuses(code, change):
