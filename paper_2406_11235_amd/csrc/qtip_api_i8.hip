@@ -130,10 +130,10 @@ int qtip_norm_residual(const void *y, int64_t ldy, int y_type, const void *h, in
 }
 
 size_t qtip_moe_i8_workspace(int T, int n, int f, int E, int top_k) {
-    if (T < 1 || T > QTIP_MOE_MAX_TOKENS || n < 1 || f < 1 || f > QTIP_ROWS_MAX_N || E < 1 || E > QTIP_MOE_MAX_EXPERTS ||
+    if (T < 1 || T > QTIP_MOE_MAX_TOKENS || n < 1 || n > QTIP_ROWS_MAX_N || f < 1 || f > QTIP_ROWS_MAX_N || E < 1 || E > QTIP_MOE_MAX_EXPERTS ||
         top_k < 1 || top_k > QTIP_MOE_MAX_TOP_K || top_k > E)
         return 0;
-    return qtip::moe_i8_workspace(T, f, E, top_k);
+    return qtip::moe_i8_workspace(T, n, f, E, top_k);
 }
 
 int qtip_moe_i8(const void *x, int64_t ldx, int type, int T, int n, const void *router, const float *router_bias, int E,
@@ -155,12 +155,14 @@ int qtip_moe_i8(const void *x, int64_t ldx, int type, int T, int n, const void *
     if (n > QTIP_ROWS_MAX_N || f > QTIP_ROWS_MAX_N)
         return fail(QTIP_EINVAL, "%s: n = %d or f = %d is above QTIP_ROWS_MAX_N = %d", fn, n, f, QTIP_ROWS_MAX_N);
     if (ldx < n || ldy < n) return fail(QTIP_EINVAL, "%s: rows of x and y are less than n = %d values apart", fn, n);
+    if (ldx > QTIP_I8_MAX_LD)
+        return fail(QTIP_EINVAL, "%s: rows of x are more than QTIP_I8_MAX_LD = %d values apart", fn, QTIP_I8_MAX_LD);
     if (ldx % 8 || !aligned(x, 16) || !aligned(router, 16) || !aligned(W_up, 16) || !aligned(W_down, 16) ||
         !aligned(up_scale, 16) || !aligned(down_scale, 16))
         return fail(QTIP_EINVAL, "%s: rows of x, the router, weights and scales must begin at multiples of 16 bytes", fn);
     if (!aligned(y, 2) || !aligned(ids, 4) || !aligned(weights, 4) || !aligned(router_bias, 4) || !aligned(workspace, 256))
         return fail(QTIP_EINVAL, "%s: y needs 2-byte, ids, weights and router_bias 4-byte, workspace 256-byte alignment", fn);
-    const size_t need = qtip::moe_i8_workspace(T, f, E, top_k);
+    const size_t need = qtip::moe_i8_workspace(T, n, f, E, top_k);
     if (workspace_bytes < need) return fail(QTIP_EINVAL, "%s: workspace of %zu bytes, %zu needed", fn, workspace_bytes, need);
     hipError_t e = qtip::launch_moe_i8({x, router, router_bias, W_up, W_down, up_scale, down_scale, y, ids, weights, ldx, ldy, type,
                                         T, n, f, E, top_k, renormalize}, workspace, (hipStream_t)stream);

@@ -108,7 +108,7 @@ struct MoeI8 {
     int64_t ldx, ldy;
     int type, T, n, f, E, top_k, renormalize;
 };
-size_t moe_i8_workspace(int T, int f, int E, int top_k);
+size_t moe_i8_workspace(int T, int n, int f, int E, int top_k);
 hipError_t launch_moe_i8(const MoeI8 &a, void *ws, hipStream_t st);
 
 }  // namespace qtip
