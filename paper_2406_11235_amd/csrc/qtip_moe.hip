@@ -19,31 +19,36 @@ namespace {
 
 typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
 
-// What the choice leaves for the products, in the workspace.
+// The choice, by expert: in the workspace for the launches behind it, in LDS while it is made.
 struct Plan {
-    int experts;                               // that any token chose, ascending in expert[]
+    int experts;                       // that any token chose, ascending in expert[]
     int expert[MOE_MAX_EXPERTS];
-    int first[MOE_MAX_EXPERTS];                // its first pair (a token that chose it); pairs ascend by token
-    uint64_t tokens[MOE_MAX_EXPERTS];          // one bit for each token
-    float weight[MOE_MAX_TOKENS * MOE_MAX_TOP_K];  // by token and choice
-    int token[MOE_MAX_TOKENS * MOE_MAX_TOP_K];
-    int pair[MOE_MAX_TOKENS * MOE_MAX_TOP_K];  // by token and choice; -1: left out
+    int first[MOE_MAX_EXPERTS];        // its first pair (a token that chose it); pairs ascend by token
+    uint64_t tokens[MOE_MAX_EXPERTS];  // one bit for each token
+};
+// And by token and choice.
+struct Choice {
+    float weight;
+    int pair;  // -1: left out
 };
 
 constexpr size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 
 struct Workspace {
     Plan *plan;
-    float *logits;  // T x E
-    bf16_t *h;      // pairs x 2 x f: a row of h rounded, and one of what that left
-    float *parts;   // pairs x n: D h
+    Choice *choices;  // T x top_k
+    float *logits;    // T x E
+    bf16_t *h;        // pairs x 2 x f: a row of h rounded, and one of what that left
+    float *parts;     // pairs x n: D h
     static size_t bytes(int T, int n, int f, int E, int top_k) {
-        return round_up(sizeof(Plan)) + round_up((size_t)T * E * 4) + round_up((size_t)T * top_k * f * 4) + round_up((size_t)T * top_k * n * 4);
+        return round_up(sizeof(Plan)) + round_up((size_t)T * top_k * sizeof(Choice)) + round_up((size_t)T * E * 4) + round_up((size_t)T * top_k * f * 4) + round_up((size_t)T * top_k * n * 4);
     }
     Workspace(void *at, const MoeI8 &a) {
         char *p = (char *)at;
         plan = (Plan *)p;
         p += round_up(sizeof(Plan));
+        choices = (Choice *)p;
+        p += round_up((size_t)a.T * a.top_k * sizeof(Choice));
         logits = (float *)p;
         p += round_up((size_t)a.T * a.E * 4);
         h = (bf16_t *)p;
@@ -52,142 +57,160 @@ struct Workspace {
     }
 };
 
-// A wave: the logits of one expert for up to four tokens.
+// The logits of one expert for up to four tokens: the waves of a workgroup take 512 inputs in turn.
 template <class T> __global__ __launch_bounds__(256) void moe_logits_kernel(MoeI8 a, float *__restrict__ logits) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int e = blockIdx.x * 4 + wave, t0 = blockIdx.y * 4;
-    if (e >= a.E) return;
+    typedef T T8 __attribute__((ext_vector_type(8)));
+    __shared__ float s_sum[4][4];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int e = blockIdx.x, t0 = blockIdx.y * 4;
     const T *r = (const T *)a.router + (int64_t)e * a.n;
     const T *x[4];
 #pragma unroll
     for (int t = 0; t < 4; t++) x[t] = (const T *)a.x + (int64_t)min(t0 + t, a.T - 1) * a.ldx;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 4 * lane; k < a.n; k += 256) {
-        const float4_t w = widen(load_quad(r, k, a.n));
+#pragma unroll 2
+    for (int k = 512 * wave + 8 * lane; k < a.n; k += 2048) {  // (n is a multiple of 16)
+        const T8 w = *reinterpret_cast<const T8 *>(r + k);
+        T8 v[4];
 #pragma unroll
-        for (int t = 0; t < 4; t++) {
-            const float4_t v = widen(load_quad(x[t], k, a.n));
-            sum[t] += (w[0] * v[0] + w[1] * v[1]) + (w[2] * v[2] + w[3] * v[3]);
-        }
+        for (int t = 0; t < 4; t++) v[t] = *reinterpret_cast<const T8 *>(x[t] + k);
+#pragma unroll
+        for (int t = 0; t < 4; t++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) sum[t] += (float)w[i] * (float)v[t][i];
     }
 #pragma unroll
     for (int t = 0; t < 4; t++) {
-        const float l = wave_sum(sum[t]);
-        if (lane == 0 && t0 + t < a.T) logits[(t0 + t) * a.E + e] = l + (a.router_bias ? a.router_bias[e] : 0.f);
+        sum[t] = wave_sum(sum[t]);
+        if (lane == 0) s_sum[t][wave] = sum[t];
+    }
+    __syncthreads();
+    if (threadIdx.x < 4 && t0 + (int)threadIdx.x < a.T) {
+        const int t = threadIdx.x;
+        const float l = (s_sum[t][0] + s_sum[t][1]) + (s_sum[t][2] + s_sum[t][3]);
+        logits[(t0 + t) * a.E + e] = l + (a.router_bias ? a.router_bias[e] : 0.f);
     }
 }
 
-// One workgroup of 16 waves: each takes tokens in turn.
-__global__ __launch_bounds__(1024) void moe_choose_kernel(MoeI8 a, Workspace ws) {
-    __shared__ unsigned long long s_tokens[MOE_MAX_EXPERTS];
-    __shared__ int s_first[MOE_MAX_EXPERTS];
+// The choice by a workgroup of WAVES waves, which take tokens in turn.  plan is left whole; what goes to memory is written where
+// `write` says so.  (Loops are kept as loops: the code runs once, and fetching it is much of the time that takes: MEASURED.)
+struct ChoiceLds {
+    Plan plan;
+    unsigned long long tokens[MOE_MAX_EXPERTS];  // of all experts, chosen or not
+    int first[MOE_MAX_EXPERTS];
+    int id[MOE_MAX_TOKENS * MOE_MAX_TOP_K];
+    float weight[MOE_MAX_TOKENS * MOE_MAX_TOP_K];
+};
+template <int WAVES> __device__ __forceinline__ void choose(const MoeI8 &a, const Workspace &ws, ChoiceLds &s, bool write) {
+    constexpr int PER = MOE_MAX_EXPERTS / 64;  // experts of a lane
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (threadIdx.x < MOE_MAX_EXPERTS) s_tokens[threadIdx.x] = 0;
+    for (int e = threadIdx.x; e < a.E; e += WAVES * 64) s.tokens[e] = 0;
     __syncthreads();
-    // of the wave's tokens wave, wave + 16, ...: lane i has the i-th choice
-    constexpr int MINE = MOE_MAX_TOKENS / 16;
-    int my_id[MINE];
-    float my_weight[MINE];
-#pragma unroll
-    for (int m = 0; m < MINE; m++) {
-        const int t = wave + 16 * m;
-        my_id[m] = 0;
-        my_weight[m] = 0.f;
-        if (t >= a.T) break;
+#pragma unroll 1
+    for (int t = wave; t < a.T; t += WAVES) {
         // logits as whole numbers of the same order: NaN below everything, 0 for what is taken or not there
-        float l[MOE_MAX_EXPERTS / 64];
-        uint32_t key[MOE_MAX_EXPERTS / 64], best = 0;
+        float l[PER];
+        uint32_t key[PER], best = 0;
         bool nan = false;
 #pragma unroll
-        for (int i = 0; i < MOE_MAX_EXPERTS / 64; i++) {
-            const int e = 64 * i + lane;
-            l[i] = e < a.E ? ws.logits[t * a.E + e] : -__builtin_inff();
+        for (int i = 0; i < PER; i++) l[i] = 64 * i + lane < a.E ? ws.logits[t * a.E + 64 * i + lane] : -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
             const uint32_t bits = __builtin_bit_cast(uint32_t, l[i]);
-            key[i] = e >= a.E ? 0u : l[i] != l[i] ? 1u : bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+            key[i] = 64 * i + lane >= a.E ? 0u : l[i] != l[i] ? 1u : bits & 0x80000000u ? ~bits : bits | 0x80000000u;
             nan |= l[i] != l[i];
             best = max(best, key[i]);
         }
-        nan = __any(nan);
         best = wave_max(best);
         const uint32_t top_bits = best & 0x80000000u ? best & 0x7FFFFFFFu : ~best;
         const float top = __builtin_bit_cast(float, top_bits);
         // exp(l - top): nothing where every expert is masked
         const bool none = top == -__builtin_inff();
-        float all = 0.f, chosen = 0.f;
+        float p[PER], all = 0.f, chosen = 0.f, mine = 0.f;
 #pragma unroll
-        for (int i = 0; i < MOE_MAX_EXPERTS / 64; i++) all += none ? 0.f : __expf(l[i] - top);
-        all = wave_sum(all);
-        float mine = 0.f;
+        for (int i = 0; i < PER; i++) {
+            p[i] = none ? 0.f : __expf(l[i] - top);
+            all += p[i];
+        }
+        int id = 0;  // lane j has the j-th choice
+        uint32_t high = best;
+#pragma unroll 1
         for (int j = 0; j < a.top_k; j++) {
-            uint32_t high = 0;
+            int found = -1;
+            float w = 0.f;
 #pragma unroll
-            for (int i = 0; i < MOE_MAX_EXPERTS / 64; i++) high = max(high, key[i]);
-            high = wave_max(high);
-            int id = -1;
-            float value = 0.f;
-#pragma unroll
-            for (int i = 0; i < MOE_MAX_EXPERTS / 64; i++) {
+            for (int i = 0; i < PER; i++) {
                 const uint64_t who = __ballot(key[i] == high);
-                if (id < 0 && who) {
+                if (found < 0 && who) {
                     const int at = __builtin_ctzll(who);
-                    id = 64 * i + at;
-                    value = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, l[i]), at));
+                    found = 64 * i + at;
+                    w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, p[i]), at));
                     if (lane == at) key[i] = 0;
                 }
             }
-            const float w = none ? 0.f : __expf(value - top);
             chosen += w;
-            if (lane == j) {
-                my_id[m] = id;
-                mine = w;
-            }
+            id = lane == j ? found : id;
+            mine = lane == j ? w : mine;
+            high = max(max(key[0], key[1]), max(key[2], key[3]));
+            static_assert(PER == 4, "of four keys");
+            high = wave_max(high);
         }
-        const float sum = a.renormalize ? chosen : all;
-        my_weight[m] = nan ? __builtin_nanf("") : none ? 0.f : mine / sum;
+        const float sum = a.renormalize ? chosen : wave_sum(all);
+        const float weight = __any(nan) ? __builtin_nanf("") : none ? 0.f : mine / sum;
         if (lane < a.top_k) {
-            if (a.ids) a.ids[t * a.top_k + lane] = my_id[m];
-            if (a.weights) a.weights[t * a.top_k + lane] = my_weight[m];
+            s.id[t * a.top_k + lane] = id;
+            s.weight[t * a.top_k + lane] = weight;
             // (a weight of 0 leaves the expert out, a NaN does not)
-            if (my_weight[m] != 0.f) atomicOr(&s_tokens[my_id[m]], 1ull << t);
+            if (weight != 0.f) atomicOr(&s.tokens[id], 1ull << t);
         }
     }
     __syncthreads();
     // experts in a row and their pairs: sums over the experts before, 64 at a time by the first wave
     if (wave == 0) {
         int experts = 0, pairs = 0;
-        for (int i = 0; i < MOE_MAX_EXPERTS / 64; i++) {
-            const uint64_t tokens = s_tokens[64 * i + lane];
+#pragma unroll 1
+        for (int e = lane; e - lane < a.E; e += 64) {
+            const uint64_t tokens = e < a.E ? s.tokens[e] : 0;
             const int count = __builtin_popcountll(tokens);
             int before = count;  // inclusive sum over lanes
+#pragma unroll 1
             for (int d = 1; d < 64; d <<= 1) {
                 const int o = __shfl_up(before, d, 64);
-                if (lane >= d) before += o;
+                before += lane >= d ? o : 0;
             }
             const uint64_t any = __ballot(count > 0);
-            const int first = pairs + before - count;
-            s_first[64 * i + lane] = first;
+            const int first = pairs + before - count, at = experts + __builtin_popcountll(any & ((1ull << lane) - 1));
             if (count) {
-                const int at = experts + __builtin_popcountll(any & ((1ull << lane) - 1));
-                ws.plan->expert[at] = 64 * i + lane;
-                ws.plan->first[at] = first;
-                ws.plan->tokens[at] = tokens;
+                s.first[e] = first;
+                s.plan.expert[at] = e;
+                s.plan.first[at] = first;
+                s.plan.tokens[at] = tokens;
             }
             experts += __builtin_popcountll(any);
-            pairs += __shfl(before, 63, 64);
+            pairs += __builtin_amdgcn_readlane(before, 63);
         }
-        if (lane == 0) ws.plan->experts = experts;
+        if (lane == 0) s.plan.experts = experts;
     }
     __syncthreads();
-#pragma unroll
-    for (int m = 0; m < MINE; m++) {
-        const int t = wave + 16 * m;
-        if (t < a.T && lane < a.top_k) {
-            const int pair = my_weight[m] == 0.f ? -1 : s_first[my_id[m]] + __builtin_popcountll(s_tokens[my_id[m]] & ((1ull << t) - 1));
-            ws.plan->pair[t * a.top_k + lane] = pair;
-            ws.plan->weight[t * a.top_k + lane] = my_weight[m];
-            if (pair >= 0) ws.plan->token[pair] = t;
-        }
+    if (!write) return;
+    for (int u = threadIdx.x; u < s.plan.experts; u += WAVES * 64) {
+        ws.plan->expert[u] = s.plan.expert[u];
+        ws.plan->first[u] = s.plan.first[u];
+        ws.plan->tokens[u] = s.plan.tokens[u];
     }
+    if (threadIdx.x == 0) ws.plan->experts = s.plan.experts;
+    for (int c = threadIdx.x; c < a.T * a.top_k; c += WAVES * 64) {
+        const int id = s.id[c];
+        const float weight = s.weight[c];
+        if (a.ids) a.ids[c] = id;
+        if (a.weights) a.weights[c] = weight;
+        const uint64_t before = (1ull << (c / a.top_k)) - 1;
+        ws.choices[c] = Choice{weight, weight == 0.f ? -1 : s.first[id] + __builtin_popcountll(s.tokens[id] & before)};
+    }
+}
+__global__ __launch_bounds__(1024) void moe_choose_kernel(MoeI8 a, Workspace ws) {
+    __shared__ ChoiceLds s;
+    choose<16>(a, ws, s, true);
 }
 
 // Sixteen weights as two operands of eight, in the activations' type.
@@ -210,14 +233,15 @@ __device__ __forceinline__ void weights_of(i32x4_t v, typename Operand<T>::type 
     for (int d = 0; d < 4; d++)
 #pragma unroll
         for (int b = 0; b < 4; b++) {
-            const float one = (float)(int8_t)(v[d] >> (8 * b));
+            const float one = (float)(int)__builtin_amdgcn_sbfe(v[d], 8 * b, 8);  // (part of the conversion's operand)
             if (d < 2) first[4 * d + b] = (T)one;
             else second[4 * (d - 2) + b] = (T)one;
         }
 }
 
-// The waves of a workgroup and the LDS that each has to itself; two workgroups on a CU.
-constexpr int NW = 4, WAVE_LDS = 20 * 1024;
+// The waves of a workgroup, the LDS that each has to itself, and workgroups on a CU: the short work of one fills the others'
+// beginnings and ends (two with 20 KiB a wave: 16 tokens, 64 experts of 1024 x 2048, 90 us, four with 10 KiB 79).
+constexpr int NW = 4, WAVE_LDS = 10 * 1024, WGS = 4;
 
 // Two blocks of 16 rows of 8-bit weights times up to 4 XC rows of activations: sum[block][16 rows], all of them in every
 // lane's usual place.  The waves take 128 inputs in turn and add up at the end.  Each wave has a ring of stages in LDS,
@@ -322,12 +346,12 @@ __device__ __forceinline__ void expert_sums(u32x4_t buffer_w, const uint32_t (&w
     __syncthreads();
 }
 
-// All rows of activations, 32 at a time: done(block sums, number of the row) in the lanes that have a row.
+// All rows of activations, 16 at a time: done(block sums, number of the row) in the lanes that have a row.
 template <class T, class At, class Done>
 __device__ __forceinline__ void expert_rows(u32x4_t buffer_w, const uint32_t (&w_at)[2], u32x4_t buffer_x, At x_at, int rows, int n,
                                             char *s_ring, Done done) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    for (int r0 = 0; r0 < rows; r0 += 32) {
+    for (int r0 = 0; r0 < rows; r0 += 16) {
         auto some = [&](auto xc) {
             float4_t sum[2][(xc + 3) / 4];
             expert_sums<T, xc>(buffer_w, w_at, buffer_x, [&](int r) { return x_at(r0 + r); }, rows - r0, n, s_ring, sum);
@@ -336,25 +360,39 @@ __device__ __forceinline__ void expert_rows(u32x4_t buffer_w, const uint32_t (&w
         };
         if (rows - r0 <= 4) some(std::integral_constant<int, 1>{});
         else if (rows - r0 <= 8) some(std::integral_constant<int, 2>{});
-        else if (rows - r0 <= 16) some(std::integral_constant<int, 4>{});
-        else some(std::integral_constant<int, 8>{});
+        else some(std::integral_constant<int, 4>{});
     }
 }
 
-// h of 16 rows of G and U of one expert.
-template <class T> __global__ __launch_bounds__(NW * 64) void moe_up_kernel(MoeI8 a, Workspace ws) {
+// The place of the r-th set bit.
+__device__ __forceinline__ int bit_of(uint64_t bits, int r) {
+    for (; r > 0; r--) bits &= bits - 1;
+    return __builtin_ctzll(bits);
+}
+
+// h of 16 rows of G and U of one expert.  CHOOSE: for as many tokens as there are waves, every workgroup makes the choice
+// itself, which takes less than a launch (1 token, 8 experts: CHOOSE_US), and the first one writes it down.
+template <class T, bool CHOOSE> __global__ __launch_bounds__(NW * 64, WGS) void moe_up_kernel(MoeI8 a, Workspace ws) {
     __shared__ __attribute__((aligned(1024))) char s_ring[NW * WAVE_LDS];
-    const Plan &plan = *ws.plan;
     const int u = blockIdx.y;
-    if (u >= plan.experts) return;
-    const int e = plan.expert[u], first = plan.first[u], count = __builtin_popcountll(plan.tokens[u]);
+    const Plan *plan = ws.plan;
+    if constexpr (CHOOSE) {
+        ChoiceLds &s = *reinterpret_cast<ChoiceLds *>(s_ring);
+        choose<NW>(a, ws, s, blockIdx.x == 0 && u == 0);
+        plan = &s.plan;
+    }
+    if (u >= plan->experts) return;
+    const int e = plan->expert[u], first = plan->first[u];
+    const uint64_t tokens = plan->tokens[u];
+    const int count = __builtin_popcountll(tokens);
+    if constexpr (CHOOSE) __syncthreads();  // (the ring is where the choice was made)
     const int i0 = blockIdx.x * 16, i = i0 + 4 * ((threadIdx.x & 63) >> 4);
     const u32x4_t buffer_w = buffer_of(a.W_up + (int64_t)e * 2 * a.f * a.n, (size_t)2 * a.f * a.n);
     const u32x4_t buffer_x = buffer_of(a.x, ((size_t)(a.T - 1) * a.ldx + a.n) * 2);
     const uint32_t w_at[2] = {(uint32_t)i0 * a.n, (uint32_t)(a.f + i0) * a.n};
     const float4_t sg = *reinterpret_cast<const float4_t *>(a.up_scale + (int64_t)e * 2 * a.f + i);
     const float4_t su = *reinterpret_cast<const float4_t *>(a.up_scale + (int64_t)e * 2 * a.f + a.f + i);
-    expert_rows<T>(buffer_w, w_at, buffer_x, [&](int r) { return (uint32_t)plan.token[first + r] * (uint32_t)a.ldx * 2; }, count, a.n,
+    expert_rows<T>(buffer_w, w_at, buffer_x, [&](int r) { return (uint32_t)bit_of(tokens, r) * (uint32_t)a.ldx * 2; }, count, a.n,
                    s_ring, [&](float4_t g, float4_t up, int r, bool there) {
         if (!there) return;
         bf16x4_t high, low;
@@ -373,7 +411,7 @@ template <class T> __global__ __launch_bounds__(NW * 64) void moe_up_kernel(MoeI
 }
 
 // D h of 32 rows of D of one expert.
-__global__ __launch_bounds__(NW * 64) void moe_down_kernel(MoeI8 a, Workspace ws) {
+__global__ __launch_bounds__(NW * 64, WGS) void moe_down_kernel(MoeI8 a, Workspace ws) {
     __shared__ __attribute__((aligned(1024))) char s_ring[NW * WAVE_LDS];
     const Plan &plan = *ws.plan;
     const int u = blockIdx.y;
@@ -407,17 +445,21 @@ template <class T> __global__ __launch_bounds__(256) void moe_join_kernel(MoeI8 
     if (i >= a.n) return;
     float4_t y = {0.f, 0.f, 0.f, 0.f};
     for (int j = 0; j < a.top_k; j++) {
-        const int pair = ws.plan->pair[t * a.top_k + j];
-        if (pair >= 0) y += ws.plan->weight[t * a.top_k + j] * *reinterpret_cast<const float4_t *>(ws.parts + (int64_t)pair * a.n + i);
+        const Choice c = ws.choices[t * a.top_k + j];
+        if (c.pair >= 0) y += c.weight * *reinterpret_cast<const float4_t *>(ws.parts + (int64_t)c.pair * a.n + i);
     }
     store_quad((T *)a.y + t * a.ldy, i, a.n, y);
 }
 
 template <class T> void launch_moe(const MoeI8 &a, const Workspace &ws, hipStream_t st) {
-    hipLaunchKernelGGL((moe_logits_kernel<T>), dim3((a.E + 3) / 4, (a.T + 3) / 4), dim3(256), 0, st, a, ws.logits);
-    hipLaunchKernelGGL(moe_choose_kernel, dim3(1), dim3(1024), 0, st, a, ws);
+    hipLaunchKernelGGL((moe_logits_kernel<T>), dim3(a.E, (a.T + 3) / 4), dim3(256), 0, st, a, ws.logits);
     const int experts = a.T * a.top_k < a.E ? a.T * a.top_k : a.E;
-    hipLaunchKernelGGL((moe_up_kernel<T>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
+    if (a.T <= NW) {
+        hipLaunchKernelGGL((moe_up_kernel<T, true>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
+    } else {
+        hipLaunchKernelGGL(moe_choose_kernel, dim3(1), dim3(1024), 0, st, a, ws);
+        hipLaunchKernelGGL((moe_up_kernel<T, false>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
+    }
     hipLaunchKernelGGL(moe_down_kernel, dim3((a.n + 31) / 32, experts), dim3(NW * 64), 0, st, a, ws);
     hipLaunchKernelGGL((moe_join_kernel<T>), dim3((a.n + 1023) / 1024, a.T), dim3(256), 0, st, a, ws);
 }
