@@ -93,7 +93,8 @@ template <class T> __global__ __launch_bounds__(256) void moe_logits_kernel(MoeI
 }
 
 // The choice by a workgroup of WAVES waves, which take tokens in turn.  plan is left whole; what goes to memory is written where
-// `write` says so.  (Loops are kept as loops: the code runs once, and fetching it is much of the time that takes: MEASURED.)
+// `write` says so.  (Loops are kept as loops: the code runs once, and fetching it is much of the time that takes: 16 tokens, 64 experts
+// of 1024 x 2048, the whole layer, 80.8 us with the loop over tokens unrolled, 76.4 so.)
 struct ChoiceLds {
     Plan plan;
     unsigned long long tokens[MOE_MAX_EXPERTS];  // of all experts, chosen or not
@@ -239,9 +240,15 @@ __device__ __forceinline__ void weights_of(i32x4_t v, typename Operand<T>::type 
         }
 }
 
-// The waves of a workgroup, the LDS that each has to itself, and workgroups on a CU: the short work of one fills the others'
-// beginnings and ends (two with 20 KiB a wave: 16 tokens, 64 experts of 1024 x 2048, 90 us, four with 10 KiB 79).
-constexpr int NW = 4, WAVE_LDS = 10 * 1024, WGS = 4;
+// The waves of a workgroup, the LDS that each has to itself, and workgroups on a CU: 10 KiB and four, so that the work of one fills
+// the others' beginnings and ends (16 tokens, 64 experts of 1024 x 2048: 79 us, with 20 KiB and two 90), and 16 rows of
+// activations at a time.  WIDE, 20 KiB and two: 32 rows at a time, where an expert has many tokens and 16 rows would have its weights
+// read more often (64 tokens, us, narrow and wide: 2 of 8 experts of 14336 x 4096 443 and 364, 4 of 16 of 2048 x 4096 150 and 133,
+// 4 of 32 185 and 195; 32 tokens, 4 of 16 104 and 109).
+constexpr int NW = 4;
+template <bool WIDE> constexpr int WAVE_LDS = WIDE ? 20 * 1024 : 10 * 1024;
+template <bool WIDE> constexpr int WGS = WIDE ? 2 : 4;
+bool wide(const MoeI8 &a) { return a.T * a.top_k >= 12 * a.E; }
 
 // Two blocks of 16 rows of 8-bit weights times up to 4 XC rows of activations: sum[block][16 rows], all of them in every
 // lane's usual place.  The waves take 128 inputs in turn and add up at the end.  Each wave has a ring of stages in LDS,
@@ -249,13 +256,13 @@ constexpr int NW = 4, WAVE_LDS = 10 * 1024, WGS = 4;
 // Unit c (16 bytes) of row r is at place c ^ (r / 2 % 8) of weights, c ^ r of activations: 16 rows one after the other have the
 // same unit in different banks.
 //   w_at[b], x_at(r): where a block's first row and activation row r begin in their buffers (row r >= rows: zeros).
-template <class T, int XC, class At>
+template <class T, int XC, bool WIDE, class At>
 __device__ __forceinline__ void expert_sums(u32x4_t buffer_w, const uint32_t (&w_at)[2], u32x4_t buffer_x, At x_at, int rows, int n,
                                             char *s_ring, float4_t (&sum)[2][(XC + 3) / 4]) {
     typedef typename Operand<T>::type op_t;
-    constexpr int NB = (XC + 3) / 4, STAGE = (4 + XC) * 1024, D = WAVE_LDS / STAGE;
+    constexpr int NB = (XC + 3) / 4, STAGE = (4 + XC) * 1024, D = WAVE_LDS<WIDE> / STAGE;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    char *const ring = s_ring + wave * WAVE_LDS;
+    char *const ring = s_ring + wave * WAVE_LDS<WIDE>;
     uint32_t at_w[4], at_x[XC];
     int k_x[XC];  // the first input that the lane copies of activations
 #pragma unroll
@@ -346,21 +353,22 @@ __device__ __forceinline__ void expert_sums(u32x4_t buffer_w, const uint32_t (&w
     __syncthreads();
 }
 
-// All rows of activations, 16 at a time: done(block sums, number of the row) in the lanes that have a row.
-template <class T, class At, class Done>
+// All rows of activations, 16 or 32 at a time: done(block sums, number of the row) in the lanes that have a row.
+template <class T, bool WIDE, class At, class Done>
 __device__ __forceinline__ void expert_rows(u32x4_t buffer_w, const uint32_t (&w_at)[2], u32x4_t buffer_x, At x_at, int rows, int n,
                                             char *s_ring, Done done) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    for (int r0 = 0; r0 < rows; r0 += 16) {
+    for (int r0 = 0; r0 < rows; r0 += WIDE ? 32 : 16) {
         auto some = [&](auto xc) {
             float4_t sum[2][(xc + 3) / 4];
-            expert_sums<T, xc>(buffer_w, w_at, buffer_x, [&](int r) { return x_at(r0 + r); }, rows - r0, n, s_ring, sum);
+            expert_sums<T, xc, WIDE>(buffer_w, w_at, buffer_x, [&](int r) { return x_at(r0 + r); }, rows - r0, n, s_ring, sum);
             const int r = 16 * wave + (lane & 15);
             if (wave < (xc + 3) / 4) done(sum[0][0], sum[1][0], r0 + r, r < 4 * xc && r0 + r < rows);
         };
         if (rows - r0 <= 4) some(std::integral_constant<int, 1>{});
         else if (rows - r0 <= 8) some(std::integral_constant<int, 2>{});
-        else some(std::integral_constant<int, 4>{});
+        else if (!WIDE || rows - r0 <= 16) some(std::integral_constant<int, 4>{});
+        else if constexpr (WIDE) some(std::integral_constant<int, 8>{});
     }
 }
 
@@ -371,9 +379,10 @@ __device__ __forceinline__ int bit_of(uint64_t bits, int r) {
 }
 
 // h of 16 rows of G and U of one expert.  CHOOSE: for as many tokens as there are waves, every workgroup makes the choice
-// itself, which takes less than a launch (1 token, 8 experts: CHOOSE_US), and the first one writes it down.
-template <class T, bool CHOOSE> __global__ __launch_bounds__(NW * 64, WGS) void moe_up_kernel(MoeI8 a, Workspace ws) {
-    __shared__ __attribute__((aligned(1024))) char s_ring[NW * WAVE_LDS];
+// itself, which takes less than a launch (1 token, 2 of 8 experts of 14336 x 4096: 78.3 us, with a launch 79.9), and the first
+// one writes it down.
+template <class T, bool CHOOSE, bool WIDE> __global__ __launch_bounds__(NW * 64, WGS<WIDE>) void moe_up_kernel(MoeI8 a, Workspace ws) {
+    __shared__ __attribute__((aligned(1024))) char s_ring[NW * WAVE_LDS<WIDE>];
     const int u = blockIdx.y;
     const Plan *plan = ws.plan;
     if constexpr (CHOOSE) {
@@ -392,7 +401,7 @@ template <class T, bool CHOOSE> __global__ __launch_bounds__(NW * 64, WGS) void 
     const uint32_t w_at[2] = {(uint32_t)i0 * a.n, (uint32_t)(a.f + i0) * a.n};
     const float4_t sg = *reinterpret_cast<const float4_t *>(a.up_scale + (int64_t)e * 2 * a.f + i);
     const float4_t su = *reinterpret_cast<const float4_t *>(a.up_scale + (int64_t)e * 2 * a.f + a.f + i);
-    expert_rows<T>(buffer_w, w_at, buffer_x, [&](int r) { return (uint32_t)bit_of(tokens, r) * (uint32_t)a.ldx * 2; }, count, a.n,
+    expert_rows<T, WIDE>(buffer_w, w_at, buffer_x, [&](int r) { return (uint32_t)bit_of(tokens, r) * (uint32_t)a.ldx * 2; }, count, a.n,
                    s_ring, [&](float4_t g, float4_t up, int r, bool there) {
         if (!there) return;
         bf16x4_t high, low;
@@ -411,8 +420,8 @@ template <class T, bool CHOOSE> __global__ __launch_bounds__(NW * 64, WGS) void 
 }
 
 // D h of 32 rows of D of one expert.
-__global__ __launch_bounds__(NW * 64, WGS) void moe_down_kernel(MoeI8 a, Workspace ws) {
-    __shared__ __attribute__((aligned(1024))) char s_ring[NW * WAVE_LDS];
+template <bool WIDE> __global__ __launch_bounds__(NW * 64, WGS<WIDE>) void moe_down_kernel(MoeI8 a, Workspace ws) {
+    __shared__ __attribute__((aligned(1024))) char s_ring[NW * WAVE_LDS<WIDE>];
     const Plan &plan = *ws.plan;
     const int u = blockIdx.y;
     if (u >= plan.experts) return;
@@ -423,7 +432,7 @@ __global__ __launch_bounds__(NW * 64, WGS) void moe_down_kernel(MoeI8 a, Workspa
     const uint32_t w_at[2] = {(uint32_t)i0 * a.f, (uint32_t)i1 * a.f};
     const float4_t s0 = *reinterpret_cast<const float4_t *>(a.down_scale + (int64_t)e * a.n + i);
     const float4_t s1 = *reinterpret_cast<const float4_t *>(a.down_scale + (int64_t)e * a.n + i1 + (i - i0));
-    expert_rows<bf16_t>(buffer_w, w_at, buffer_x, [&](int r) { return (uint32_t)r * (uint32_t)a.f * 2; }, 2 * count, a.f, s_ring,
+    expert_rows<bf16_t, WIDE>(buffer_w, w_at, buffer_x, [&](int r) { return (uint32_t)r * (uint32_t)a.f * 2; }, 2 * count, a.f, s_ring,
                         [&](float4_t d0, float4_t d1, int r, bool there) {
         // (the two rows of one h are in neighbouring lanes)
 #pragma unroll
@@ -455,12 +464,14 @@ template <class T> void launch_moe(const MoeI8 &a, const Workspace &ws, hipStrea
     hipLaunchKernelGGL((moe_logits_kernel<T>), dim3(a.E, (a.T + 3) / 4), dim3(256), 0, st, a, ws.logits);
     const int experts = a.T * a.top_k < a.E ? a.T * a.top_k : a.E;
     if (a.T <= NW) {
-        hipLaunchKernelGGL((moe_up_kernel<T, true>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
+        hipLaunchKernelGGL((moe_up_kernel<T, true, false>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
     } else {
         hipLaunchKernelGGL(moe_choose_kernel, dim3(1), dim3(1024), 0, st, a, ws);
-        hipLaunchKernelGGL((moe_up_kernel<T, false>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
+        if (wide(a)) hipLaunchKernelGGL((moe_up_kernel<T, false, true>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
+        else hipLaunchKernelGGL((moe_up_kernel<T, false, false>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
     }
-    hipLaunchKernelGGL(moe_down_kernel, dim3((a.n + 31) / 32, experts), dim3(NW * 64), 0, st, a, ws);
+    if (wide(a)) hipLaunchKernelGGL((moe_down_kernel<true>), dim3((a.n + 31) / 32, experts), dim3(NW * 64), 0, st, a, ws);
+    else hipLaunchKernelGGL((moe_down_kernel<false>), dim3((a.n + 31) / 32, experts), dim3(NW * 64), 0, st, a, ws);
     hipLaunchKernelGGL((moe_join_kernel<T>), dim3((a.n + 1023) / 1024, a.T), dim3(256), 0, st, a, ws);
 }
 
