@@ -19,35 +19,40 @@ __device__ __forceinline__ float4_t widen(float4_t v) { return v; }
 __device__ __forceinline__ float4_t widen(half4_t v) { return __builtin_convertvector(v, float4_t); }
 __device__ __forceinline__ float4_t widen(bf16x4_t v) { return __builtin_convertvector(v, float4_t); }
 
-// Values at ... at + 3 of a row of n; zeros beyond its end.
-template <class T> __device__ __forceinline__ typename Quad<T>::type load_quad(const T *row, int at, int n) {
-    typename Quad<T>::type v = {(T)0.f, (T)0.f, (T)0.f, (T)0.f};
-    if (at + 4 <= n) {
-        v = *reinterpret_cast<const typename Quad<T>::anywhere *>(row + at);
-    } else if (at < n) {
-        v[0] = row[at];
-        if (at + 1 < n) v[1] = row[at + 1];
-        if (at + 2 < n) v[2] = row[at + 2];
+// Values at ... at + 3 of a row of n; zeros beyond its end.  RAGGED: n may be any number, else it is a multiple of four.
+// (Offsets of 32 bits from a place that all lanes share take one register where an address takes two.)
+template <bool RAGGED = true, class T> __device__ __forceinline__ typename Quad<T>::type load_quad(const T *row, int at, int n) {
+    typedef typename Quad<T>::type quad_t;
+    quad_t v = {(T)0.f, (T)0.f, (T)0.f, (T)0.f};
+    const char *const p = reinterpret_cast<const char *>(row) + (uint32_t)at * (uint32_t)sizeof(T);
+    if (RAGGED ? at + 4 <= n : at < n) {
+        v = *reinterpret_cast<const typename Quad<T>::anywhere *>(p);
+    } else if (RAGGED && at < n) {
+        v[0] = reinterpret_cast<const T *>(p)[0];
+        if (at + 1 < n) v[1] = reinterpret_cast<const T *>(p)[1];
+        if (at + 2 < n) v[2] = reinterpret_cast<const T *>(p)[2];
     }
     return v;
 }
-template <class T> __device__ __forceinline__ void store_quad(T *row, int at, int n, float4_t v) {
+template <bool RAGGED = true, class T> __device__ __forceinline__ void store_quad(T *row, int at, int n, float4_t v) {
     const typename Quad<T>::type r = __builtin_convertvector(v, typename Quad<T>::type);
-    if (at + 4 <= n) {
-        *reinterpret_cast<typename Quad<T>::anywhere *>(row + at) = r;
-    } else if (at < n) {
-        row[at] = r[0];
-        if (at + 1 < n) row[at + 1] = r[1];
-        if (at + 2 < n) row[at + 2] = r[2];
+    char *const p = reinterpret_cast<char *>(row) + (uint32_t)at * (uint32_t)sizeof(T);
+    if (RAGGED ? at + 4 <= n : at < n) {
+        *reinterpret_cast<typename Quad<T>::anywhere *>(p) = r;
+    } else if (RAGGED && at < n) {
+        reinterpret_cast<T *>(p)[0] = r[0];
+        if (at + 1 < n) reinterpret_cast<T *>(p)[1] = r[1];
+        if (at + 2 < n) reinterpret_cast<T *>(p)[2] = r[2];
     }
 }
 // Four bytes in a word, the first one lowest.
-__device__ __forceinline__ void store_quad(int8_t *row, int at, int n, uint32_t word) {
+template <bool RAGGED = true> __device__ __forceinline__ void store_quad(int8_t *row, int at, int n, uint32_t word) {
     typedef uint32_t anywhere __attribute__((aligned(1)));
-    if (at + 4 <= n) {
-        *reinterpret_cast<anywhere *>(row + at) = word;
-    } else {
-        for (int r = 0; at + r < n; r++) row[at + r] = (int8_t)(word >> (8 * r));
+    int8_t *const p = row + (uint32_t)at;
+    if (RAGGED ? at + 4 <= n : at < n) {
+        *reinterpret_cast<anywhere *>(p) = word;
+    } else if (RAGGED) {
+        for (int r = 0; at + r < n; r++) p[r] = (int8_t)(word >> (8 * r));
     }
 }
 
@@ -75,24 +80,30 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
     auto row = [&](int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); };
     return max(max(row(0), row(16)), max(row(32), row(48)));
 }
-// Over NW waves; `slots` is used by no other exchange of the kernel.
-template <int NW> __device__ __forceinline__ float block_sum(float v, float *slots) {
+// Over the workgroup's waves, at most 16, which all make the call: every lane has it.  `slots`: 16 of them, that another exchange
+// may use once every wave has been at a barrier behind this call.
+__device__ __forceinline__ float block_sum(float v, float *slots, int waves) {
     v = wave_sum(v);
     if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
     __syncthreads();
-    float t = 0.f;
-#pragma unroll
-    for (int w = 0; w < NW; w++) t += slots[w];
+    const int l = threadIdx.x & 15;
+    float t = l < waves ? slots[l] : 0.f;
+    t += __builtin_bit_cast(float, dpp<0xB1>(__builtin_bit_cast(uint32_t, t)));
+    t += __builtin_bit_cast(float, dpp<0x4E>(__builtin_bit_cast(uint32_t, t)));
+    t += __builtin_bit_cast(float, dpp<0x141>(__builtin_bit_cast(uint32_t, t)));
+    t += __builtin_bit_cast(float, dpp<0x140>(__builtin_bit_cast(uint32_t, t)));
     return t;
 }
-template <int NW> __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t *slots) {
+__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t *slots, int waves) {
     v = wave_max(v);
     if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
     __syncthreads();
-    uint32_t t = 0;
-#pragma unroll
-    for (int w = 0; w < NW; w++) t = max(t, slots[w]);
-    return t;
+    const int l = threadIdx.x & 15;
+    uint32_t t = l < waves ? slots[l] : 0u;
+    t = max(t, dpp<0xB1>(t));
+    t = max(t, dpp<0x4E>(t));
+    t = max(t, dpp<0x141>(t));
+    return max(t, dpp<0x140>(t));
 }
 
 }  // namespace qtip
