@@ -15,60 +15,147 @@ namespace qtip {
 
 namespace {
 
-// Where a thread's quad number q lies in its row.  Rotated rows: chunks of 4096 by 16 waves, as rht_chunk takes
-// (in) and leaves (out) them.
+// Where a thread's quad number q lies in its row.  Rotated rows: a wave has 1024 neighbouring values (and, of rows above
+// 16384, 1024 more 16 waves on), a lane four quads of them 256 apart; which of 16 quads next to each other says rht_lane_t.
 template <bool ROT> __device__ __forceinline__ int quad_in(int q) {
-    if constexpr (ROT) return q * RHT_CHUNK + rht_in_index(threadIdx.x >> 6, threadIdx.x & 63);
-    else return 4 * (q * (int)blockDim.x + (int)threadIdx.x);
+    if constexpr (ROT) {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        return 1024 * (wave + 16 * (q >> 2)) + 256 * (q & 3) + 64 * (lane >> 4) + 4 * rht_lane_t(lane & 15);
+    } else {
+        return 4 * (q * (int)blockDim.x + (int)threadIdx.x);
+    }
 }
-template <bool ROT> __device__ __forceinline__ int quad_out(int q) {
-    if constexpr (ROT) return q * RHT_CHUNK + rht_out_index(threadIdx.x >> 6, threadIdx.x & 63);
-    else return 4 * (q * (int)blockDim.x + (int)threadIdx.x);
+// Where it lies when the row is rotated: quad q at base + first for q & 1 + second for q & 2.
+struct Places {
+    int base, first, second;
+};
+template <bool ROT> __device__ __forceinline__ int quad_out(const Places &o, int q) {
+    if constexpr (ROT) return o.base + (q & 1 ? o.first : 0) + (q & 2 ? o.second : 0) + (q >> 2) * 16384;
+    else return quad_in<false>(q);
 }
 
-// v: quads at quad_in() to quads at quad_out() of V (S .* v), blocks of 2^p values.
-template <int Q>
-__device__ __forceinline__ void rotate_row(float4_t (&v)[Q], const int8_t *__restrict__ signs, int n, int p, float *s_v) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    uint32_t s[Q];
+// Four quads' butterflies over one bit of the quad's number.
+__device__ __forceinline__ void quad_stage(float4_t &a, float4_t &b) {
+    const float4_t t = a;
+    a = t + b;
+    b = t - b;
+}
+// One stage over lanes, PATTERN the DPP form that brings a lane its partner: mine + other in the lower lane, mine - other in the
+// upper one, the negative of what a butterfly has there.  `sign` is 1 and -1; the negative signs are made up for afterwards.  (An
+// instruction for each value; the compiler takes two.  What DPP reads has to be written two instructions before: the s_nop.)
+#define QTIP_LANE_STAGE(v, sign, PATTERN)                                                                             \
+    asm("s_nop 1\n\t"                                                                                                 \
+        "v_fmac_f32_dpp %0, %0, %4 " PATTERN " row_mask:0xf bank_mask:0xf\n\t"                                        \
+        "v_fmac_f32_dpp %1, %1, %4 " PATTERN " row_mask:0xf bank_mask:0xf\n\t"                                        \
+        "v_fmac_f32_dpp %2, %2, %4 " PATTERN " row_mask:0xf bank_mask:0xf\n\t"                                        \
+        "v_fmac_f32_dpp %3, %3, %4 " PATTERN " row_mask:0xf bank_mask:0xf"                                            \
+        : "+v"(v##0), "+v"(v##1), "+v"(v##2), "+v"(v##3)                                                              \
+        : "v"(sign))
+// One stage over lane bit 5 (WIDE) or 4: what is in the upper lanes of a changes places with what is in the lower ones of b, and
+// the stage is one between registers; lanes take over the bit that told a from b.
+template <bool WIDE> __device__ __forceinline__ void swap_stage(float4_t &a, float4_t &b, bool add) {
+    typedef uint32_t two_t __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int q = 0; q < Q; q++) {
-        const int at = quad_in<true>(q);
+    for (int r = 0; r < 4; r++) {
+        const float x = a[r], y = b[r];
+        two_t t;
+        if constexpr (WIDE) t = __builtin_bit_cast(two_t, __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false));
+        else t = __builtin_bit_cast(two_t, __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false));
+        const uint32_t t0 = t[0], t1 = t[1];
+        a[r] = __builtin_bit_cast(float, t0);
+        b[r] = __builtin_bit_cast(float, t1);
+    }
+    if (add) quad_stage(a, b);
+}
+
+// v: quads at quad_in() to quads at quad_out() of V (S .* v), blocks of 2^p values.  A value's place has bits 0-1 in a quad, 2-5 over the 16
+// lanes of a row (basis 1, 2, 7, 15: rht_lane_t), 6-7 over rows of lanes, 8-9 over the lane's quads and the rest over waves: each
+// stage is between registers, through DPP, or between registers behind an exchange; two bits of the wave's number at a time change
+// places with the quad's through LDS.  Called by whole workgroups.  `half`: the four quads' number.  s_v: 1024 floats a wave.
+__device__ __forceinline__ Places rotate_quads(float4_t (&v)[4], int half, const int8_t *__restrict__ signs, int n, int p, float4_t *s_v) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, t = rht_lane_t(lane & 15);
+    uint32_t s[4];
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+        const int at = quad_in<true>(4 * half + q);
         s[q] = at < n ? *reinterpret_cast<const uint32_t *>(signs + at) : 0u;
     }
-    RhtMatrix M;
-    M.init(lane);
-    const float scale = rht_scale(p);
+    const float s1 = t & 1 ? -1.f : 1.f, s2 = t & 2 ? -1.f : 1.f, s4 = t & 4 ? -1.f : 1.f, s8 = t & 8 ? -1.f : 1.f;
+    float scale = rht_scale(p) * s1 * s2;
+    if (p > 4) scale *= s4;
+    if (p > 5) scale *= s8;
 #pragma unroll
-    for (int q = 0; q < Q; q++) {
-        if (q * RHT_CHUNK >= n) break;
-        const float4_t in[1] = {rht_signed(v[q], s[q])};
-        float4_t out[1];
-        rht_chunk<16>(in, M, p, 16, s_v + (q & 1) * RHT_LDS_FLOATS, wave, lane, out);
-        v[q] = out[0];
+    for (int q = 0; q < 4; q++) {
+        const float4_t x = rht_signed(v[q], s[q]);
+        const float a = x[0] + x[1], b = x[0] - x[1], c = x[2] + x[3], d = x[2] - x[3];
+        float y0 = a + c, y1 = b + d, y2 = a - c, y3 = b - d;
+        QTIP_LANE_STAGE(y, s1, "quad_perm:[1,0,3,2]");
+        QTIP_LANE_STAGE(y, s2, "quad_perm:[2,3,0,1]");
+        if (p > 4) QTIP_LANE_STAGE(y, s4, "row_half_mirror");
+        if (p > 5) QTIP_LANE_STAGE(y, s8, "row_mirror");
+        v[q] = float4_t{y0, y1, y2, y3} * scale;
     }
-    // the butterflies between the chunks of blocks of 8192 and 16384
-#pragma unroll
-    for (int h = 1; h < 4; h <<= 1) {
-        if (p < (h == 1 ? 13 : 14)) break;
-#pragma unroll
-        for (int q = 0; q < Q; q++)
-            if ((q & h) == 0 && (q | h) < Q) {
-                const float4_t a = v[q], b = v[q | h];
-                v[q] = a + b;
-                v[q | h] = a - b;
-            }
+    if (p > 8) {
+        quad_stage(v[0], v[1]);
+        quad_stage(v[2], v[3]);
     }
+    if (p > 9) {
+        quad_stage(v[0], v[2]);
+        quad_stage(v[1], v[3]);
+    }
+    swap_stage<true>(v[0], v[1], p > 7);
+    swap_stage<true>(v[2], v[3], p > 7);
+    swap_stage<false>(v[0], v[2], p > 6);
+    swap_stage<false>(v[1], v[3], p > 6);
+    const int base = 4 * t + 256 * (lane >> 5) + 512 * ((lane >> 4) & 1);
+    if (p <= 10) return Places{base + 1024 * wave, 128, 64};
+    // Quads against the waves of a group of two or four, which differ in the bits of their number from `low` on: this wave
+    // takes the quads that have its own bits from each of them.
+    auto exchange = [&](int low, bool four) {
+        __syncthreads();
 #pragma unroll
-    for (int q = 0; q < Q; q++) v[q] *= scale;
+        for (int q = 0; q < 4; q++) s_v[(wave * 4 + q) * 64 + lane] = v[q];
+        __syncthreads();
+        const int mask = four ? 3 : 1, mine = (wave >> low) & mask, rest = wave & ~(mask << low);
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const int from = rest | ((four ? q : q >> 1) << low), quad = four ? mine : 2 * mine + (q & 1);
+            v[q] = s_v[(from * 4 + quad) * 64 + lane];
+        }
+        quad_stage(v[0], v[2]);
+        quad_stage(v[1], v[3]);
+        if (four) {
+            quad_stage(v[0], v[1]);
+            quad_stage(v[2], v[3]);
+        }
+    };
+    exchange(0, p > 11);
+    if (p == 11) return Places{base + 64 * (wave & 1) + 1024 * (wave & ~1), 128, 1024};
+    const int quad = base + 128 * (wave & 1) + 64 * (wave >> 1 & 1);
+    if (p == 12) return Places{quad + 1024 * (wave & ~3), 1024, 2048};
+    exchange(2, p > 13);
+    if (p == 13) return Places{quad + 2048 * (wave >> 2 & 1) + 1024 * (wave & ~7), 1024, 4096};
+    return Places{quad + 1024 * (wave >> 2 & 3), 4096, 8192};
+}
+template <int Q>
+__device__ __forceinline__ Places rotate_row(float4_t (&v)[Q], const int8_t *__restrict__ signs, int n, int p, float4_t *s_v) {
+    Places o;
+#pragma unroll
+    for (int c = 0; c < Q / 4; c++) {
+        float4_t w[4] = {v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]};
+        o = rotate_quads(w, c, signs, n, p, s_v);
+#pragma unroll
+        for (int q = 0; q < 4; q++) v[4 * c + q] = w[q];
+    }
+    return o;
 }
 
 // The bits of the largest absolute value: they order as whole numbers, NaN above infinity, so one maximum finds those too.
-template <int Q, bool ROT> __device__ __forceinline__ uint32_t largest(const float4_t (&v)[Q], int n) {
+template <int Q, bool ROT> __device__ __forceinline__ uint32_t largest(const float4_t (&v)[Q], const Places &o, int n) {
     uint32_t top = 0;
 #pragma unroll
     for (int q = 0; q < Q; q++)
-        if (quad_out<ROT>(q) < n) {
+        if (quad_out<ROT>(o, q) < n) {
 #pragma unroll
             for (int r = 0; r < 4; r++) {
                 const float one = v[q][r];
@@ -80,7 +167,7 @@ template <int Q, bool ROT> __device__ __forceinline__ uint32_t largest(const flo
 // v to 8 bits: scale = a / 127 and q = v (127 / a) to the nearest whole number, ties to even, a = `top` the row's largest absolute
 // value.  A row of zeros has the scale 0; one with an infinity or a NaN has the scale NaN, so that what is computed of it is NaN too.
 template <int Q, bool ROT, bool RAGGED>
-__device__ __forceinline__ void store_i8(const float4_t (&v)[Q], int n, int8_t *__restrict__ to, float *scale, uint32_t top) {
+__device__ __forceinline__ void store_i8(const float4_t (&v)[Q], const Places &o, int n, int8_t *__restrict__ to, float *scale, uint32_t top) {
     const float a = __builtin_bit_cast(float, top);
     const bool finite = top < 0x7F800000u;
     if (threadIdx.x == 0) *scale = finite ? a / 127.f : __builtin_nanf("");
@@ -89,7 +176,7 @@ __device__ __forceinline__ void store_i8(const float4_t (&v)[Q], int n, int8_t *
     const bool plain = finite && a >= 0x1p-120f;
 #pragma unroll
     for (int q = 0; q < Q; q++) {
-        const int at = quad_out<ROT>(q);
+        const int at = quad_out<ROT>(o, q);
         if (at >= n) continue;
         uint32_t word = 0;
         if (plain) {
@@ -111,17 +198,15 @@ __device__ __forceinline__ void store_i8(const float4_t (&v)[Q], int n, int8_t *
 }
 
 template <int Q, bool ROT, bool RAGGED>
-__device__ __forceinline__ void store_row(const float4_t (&v)[Q], int n, int type, void *x, int64_t at_row) {
+__device__ __forceinline__ void store_row(const float4_t (&v)[Q], const Places &o, int n, int type, void *x, int64_t at_row) {
 #pragma unroll
     for (int q = 0; q < Q; q++) {
-        const int at = quad_out<ROT>(q);
+        const int at = quad_out<ROT>(o, q);
         if (type == TYPE_F32) store_quad<RAGGED>((float *)x + at_row, at, n, v[q]);
         else if (type == TYPE_F16) store_quad<RAGGED>((half_t *)x + at_row, at, n, v[q]);
         else store_quad<RAGGED>((bf16_t *)x + at_row, at, n, v[q]);
     }
 }
-
-constexpr int rotate_lds(bool rot) { return rot ? 2 * RHT_LDS_FLOATS : 1; }
 
 template <class T, int Q, bool ROT, bool RAGGED> __device__ __forceinline__ void load_row(typename Quad<T>::type (&v)[Q], const T *row, int n) {
 #pragma unroll
@@ -131,7 +216,7 @@ template <class T, int Q, bool ROT, bool RAGGED>
 __global__ __launch_bounds__(1024) void quantize_rows_kernel(const T *__restrict__ x, const T *__restrict__ up, int n, int64_t ldx,
                                                              const int8_t *__restrict__ signs, int p, int8_t *__restrict__ out,
                                                              int64_t ldq, float *__restrict__ scale) {
-    __shared__ __attribute__((aligned(16))) float s_v[rotate_lds(ROT)];
+    extern __shared__ float4_t s_v[];  // 1024 floats a wave where a row is rotated over waves
     __shared__ uint32_t s_max[16];
     const int64_t row = blockIdx.x;
     typename Quad<T>::type raw[Q], raw_up[Q];
@@ -147,9 +232,10 @@ __global__ __launch_bounds__(1024) void quantize_rows_kernel(const T *__restrict
             for (int r = 0; r < 4; r++) v[q][r] = silu(v[q][r]) * u[r];
         }
     }
-    if constexpr (ROT) rotate_row<Q>(v, signs, n, p, s_v);
-    const uint32_t top = block_max(largest<Q, ROT>(v, n), s_max, blockDim.x >> 6);
-    store_i8<Q, ROT, RAGGED>(v, n, out + row * ldq, scale + row, top);
+    Places o = {};
+    if constexpr (ROT) o = rotate_row<Q>(v, signs, n, p, s_v);
+    const uint32_t top = block_max(largest<Q, ROT>(v, o, n), s_max, blockDim.x >> 6);
+    store_i8<Q, ROT, RAGGED>(v, o, n, out + row * ldq, scale + row, top);
 }
 
 // v: (v - mean) / sqrt(mean of (v - mean)^2 + eps) * weight + bias; the mean is 0 where the norm has none.  Zeros beyond n stay.
@@ -175,7 +261,7 @@ __device__ __forceinline__ void normalize(float4_t (&v)[Q], int n, float over_n,
 
 template <class TY, class TH, int Q, bool ROT, bool RAGGED>
 __global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a) {
-    __shared__ __attribute__((aligned(16))) float s_v[rotate_lds(ROT)];
+    extern __shared__ float4_t s_v[];  // 1024 floats a wave where a row is rotated over waves
     __shared__ float s_sum[4][16];
     __shared__ uint32_t s_max[16];
     const int64_t row = blockIdx.x;
@@ -217,12 +303,13 @@ __global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a) {
         normalize<Q, ROT>(v, n, over_n, a.layer, a.eps, s_sum + 2, waves);
         affine(a.pre, a.pre_bias);
     }
-    if constexpr (ROT) rotate_row<Q>(v, a.signs, n, a.p, s_v);
+    Places o = {};
+    if constexpr (ROT) o = rotate_row<Q>(v, a.signs, n, a.p, s_v);
     if (a.x_type == TYPE_I8) {
-        const uint32_t top = block_max(largest<Q, ROT>(v, n), s_max, waves);
-        store_i8<Q, ROT, RAGGED>(v, n, (int8_t *)a.x + row * a.ldx, a.x_scale + row, top);
+        const uint32_t top = block_max(largest<Q, ROT>(v, o, n), s_max, waves);
+        store_i8<Q, ROT, RAGGED>(v, o, n, (int8_t *)a.x + row * a.ldx, a.x_scale + row, top);
     } else {
-        store_row<Q, ROT, RAGGED>(v, n, a.x_type, a.x, row * a.ldx);
+        store_row<Q, ROT, RAGGED>(v, o, n, a.x_type, a.x, row * a.ldx);
     }
 }
 
@@ -237,15 +324,18 @@ int log2_of(int block) {
 // Quads of a thread, then as many waves as hold the row.  One quad while there is at most a row for each CU (the shortest way
 // from load to store), else four: more rows on a CU at a time (us, one, two, four, eight quads: norms 4096 x 8192 67.4, 67.4, 65.4,
 // 108; 997 x 5003 20.5, 20.4, 17.0, 26.0; 4096 x 4096 33.3, 26.9, 27.4, 39.1; to 8 bits 4096 x 4096 13.6, 10.7, 10.6, 10.3).
-// Rotated rows: 16 waves and whole chunks of 4096.
+// Rotated rows: four quads, eight where 16 waves do not hold the row so.
 struct Shape {
-    int quads, waves;
+    int quads, waves, lds;
 };
-static Shape shape_of(int rows, int n, bool rot) {
-    if (rot) return {n <= 4096 ? 1 : n <= 8192 ? 2 : n <= 16384 ? 4 : 8, 16};
+static Shape shape_of(int rows, int n, bool rot, int p) {
+    if (rot) {
+        const int waves = n <= 16384 ? (n + 1023) / 1024 : 16;
+        return {n <= 16384 ? 4 : 8, waves, p > 10 ? waves * 4096 : 0};
+    }
     int quads = rows <= CUS ? 1 : 4;
     while (n > 4096 * quads) quads *= 2;
-    return {quads, (n + 256 * quads - 1) / (256 * quads)};
+    return {quads, (n + 256 * quads - 1) / (256 * quads), 0};
 }
 #define QTIP_ROWS_BY_QUADS(LAUNCH, s, rot, ragged)  \
     if (s.quads == 1) LAUNCH(1, rot, ragged);       \
@@ -253,16 +343,17 @@ static Shape shape_of(int rows, int n, bool rot) {
     else if (s.quads == 4) LAUNCH(4, rot, ragged);  \
     else LAUNCH(8, rot, ragged)
 #define QTIP_ROWS_BY_SHAPE(LAUNCH, s, n, rot)                         \
-    if (rot) { QTIP_ROWS_BY_QUADS(LAUNCH, s, true, false); }          \
+    if (rot && s.quads == 4) { LAUNCH(4, true, false); }              \
+    else if (rot) { LAUNCH(8, true, false); }                         \
     else if (n % 4) { QTIP_ROWS_BY_QUADS(LAUNCH, s, false, true); }   \
     else { QTIP_ROWS_BY_QUADS(LAUNCH, s, false, false); }
 
 template <class T>
 static void launch_quantize(const void *x, const void *up, int rows, int n, int64_t ldx, const int8_t *signs, int p, int8_t *q,
                             int64_t ldq, float *scale, hipStream_t st) {
-    const Shape s = shape_of(rows, n, signs);
+    const Shape s = shape_of(rows, n, signs, p);
 #define QTIP_QUANTIZE(Q, ROT, RAGGED)                                                                                                 \
-    hipLaunchKernelGGL((quantize_rows_kernel<T, Q, ROT, RAGGED>), dim3(rows), dim3(s.waves * 64), 0, st, (const T *)x, (const T *)up, n, \
+    hipLaunchKernelGGL((quantize_rows_kernel<T, Q, ROT, RAGGED>), dim3(rows), dim3(s.waves * 64), s.lds, st, (const T *)x, (const T *)up, n, \
                        ldx, signs, p, q, ldq, scale)
     QTIP_ROWS_BY_SHAPE(QTIP_QUANTIZE, s, n, signs);
 }
@@ -277,9 +368,9 @@ hipError_t launch_quantize_rows_i8(const void *x, const void *up, int type, int 
 }
 
 template <class TY, class TH> static void launch_norm(const NormResidual &a, int rows, hipStream_t st) {
-    const Shape s = shape_of(rows, a.n, a.signs);
+    const Shape s = shape_of(rows, a.n, a.signs, a.p);
 #define QTIP_NORM(Q, ROT, RAGGED) \
-    hipLaunchKernelGGL((norm_residual_kernel<TY, TH, Q, ROT, RAGGED>), dim3(rows), dim3(s.waves * 64), 0, st, a)
+    hipLaunchKernelGGL((norm_residual_kernel<TY, TH, Q, ROT, RAGGED>), dim3(rows), dim3(s.waves * 64), s.lds, st, a)
     QTIP_ROWS_BY_SHAPE(QTIP_NORM, s, a.n, a.signs);
 }
 
