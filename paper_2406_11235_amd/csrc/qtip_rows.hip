@@ -49,7 +49,7 @@ __device__ __forceinline__ void quad_stage(float4_t &a, float4_t &b) {
         "v_fmac_f32_dpp %1, %1, %4 " PATTERN " row_mask:0xf bank_mask:0xf\n\t"                                        \
         "v_fmac_f32_dpp %2, %2, %4 " PATTERN " row_mask:0xf bank_mask:0xf\n\t"                                        \
         "v_fmac_f32_dpp %3, %3, %4 " PATTERN " row_mask:0xf bank_mask:0xf"                                            \
-        : "+v"(v##0), "+v"(v##1), "+v"(v##2), "+v"(v##3)                                                              \
+        : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3])                                                              \
         : "v"(sign))
 // One stage over lane bit 5 (WIDE) or 4: what is in the upper lanes of a changes places with what is in the lower ones of b, and
 // the stage is one between registers; lanes take over the bit that told a from b.
@@ -84,17 +84,28 @@ __device__ __forceinline__ Places rotate_quads(float4_t (&v)[4], int half, const
     float scale = rht_scale(p) * s1 * s2;
     if (p > 4) scale *= s4;
     if (p > 5) scale *= s8;
+    float x[4][4];
 #pragma unroll
     for (int q = 0; q < 4; q++) {
-        const float4_t x = rht_signed(v[q], s[q]);
-        const float a = x[0] + x[1], b = x[0] - x[1], c = x[2] + x[3], d = x[2] - x[3];
-        float y0 = a + c, y1 = b + d, y2 = a - c, y3 = b - d;
-        QTIP_LANE_STAGE(y, s1, "quad_perm:[1,0,3,2]");
-        QTIP_LANE_STAGE(y, s2, "quad_perm:[2,3,0,1]");
-        if (p > 4) QTIP_LANE_STAGE(y, s4, "row_half_mirror");
-        if (p > 5) QTIP_LANE_STAGE(y, s8, "row_mirror");
-        v[q] = float4_t{y0, y1, y2, y3} * scale;
+        const float4_t w = rht_signed(v[q], s[q]);
+        const float a = w[0] + w[1], b = w[0] - w[1], c = w[2] + w[3], d = w[2] - w[3];
+        x[q][0] = a + c;
+        x[q][1] = b + d;
+        x[q][2] = a - c;
+        x[q][3] = b - d;
+        QTIP_LANE_STAGE(x[q], s1, "quad_perm:[1,0,3,2]");
+        QTIP_LANE_STAGE(x[q], s2, "quad_perm:[2,3,0,1]");
     }
+    if (p > 4) {
+#pragma unroll
+        for (int q = 0; q < 4; q++) QTIP_LANE_STAGE(x[q], s4, "row_half_mirror");
+    }
+    if (p > 5) {
+#pragma unroll
+        for (int q = 0; q < 4; q++) QTIP_LANE_STAGE(x[q], s8, "row_mirror");
+    }
+#pragma unroll
+    for (int q = 0; q < 4; q++) v[q] = float4_t{x[q][0], x[q][1], x[q][2], x[q][3]} * scale;
     if (p > 8) {
         quad_stage(v[0], v[1]);
         quad_stage(v[2], v[3]);
@@ -269,9 +280,22 @@ __global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a) {
     const float over_n = 1.f / (float)n;
     typename Quad<TY>::type y[Q], g[Q];
     typename Quad<TH>::type h[Q];
+    // All of a row at once where that is few registers, else one matrix after the other, and more rows on a CU (us, at once and so:
+    // 1024 x 28672 with an fp32 residual 116 and 92, 8192 x 1024 15.7 and 12.9, 997 x 5003 23.1 and 17.2, 4096 x 4096 27.4 and 29.1).
+    constexpr bool AT_ONCE = Q <= 2;
+    auto load_h = [&] {
+        if (a.h) load_row<TH, Q, ROT, RAGGED>(h, (const TH *)a.h + row * a.ldh, n);
+    };
+    auto load_gate = [&] {
+        if (a.gate) load_row<TY, Q, ROT, RAGGED>(g, (const TY *)a.gate + row * a.ldgate, n);
+    };
     if (a.y) load_row<TY, Q, ROT, RAGGED>(y, (const TY *)a.y + row * a.ldy, n);
-    if (a.h) load_row<TH, Q, ROT, RAGGED>(h, (const TH *)a.h + row * a.ldh, n);
-    if (a.gate) load_row<TY, Q, ROT, RAGGED>(g, (const TY *)a.gate + row * a.ldgate, n);
+    if (AT_ONCE) {
+        load_h();
+        load_gate();
+    } else if (!a.y) {
+        load_h();
+    }
     float4_t v[Q];
     auto affine = [&](const float *weight, const float *bias) {
 #pragma unroll
@@ -286,12 +310,26 @@ __global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a) {
         normalize<Q, ROT>(v, n, over_n, a.layer, a.eps, s_sum, waves);
         affine(a.post, a.post_bias);
     }
-    if (a.y) {
+    if constexpr (AT_ONCE) {
+        if (a.y) {
+#pragma unroll
+            for (int q = 0; q < Q; q++) {
+                if (a.gate) v[q] *= widen(g[q]);
+                v[q] *= a.res_scale;
+                if (a.h) v[q] += widen(h[q]);
+            }
+        }
+    } else if (a.y) {
+        load_gate();
 #pragma unroll
         for (int q = 0; q < Q; q++) {
             if (a.gate) v[q] *= widen(g[q]);
             v[q] *= a.res_scale;
-            if (a.h) v[q] += widen(h[q]);
+        }
+        load_h();
+        if (a.h) {
+#pragma unroll
+            for (int q = 0; q < Q; q++) v[q] += widen(h[q]);
         }
     }
     if (a.h_out) {
@@ -322,8 +360,8 @@ int log2_of(int block) {
 }  // namespace
 
 // Quads of a thread, then as many waves as hold the row.  One quad while there is at most a row for each CU (the shortest way
-// from load to store), else four: more rows on a CU at a time (us, one, two, four, eight quads: norms 4096 x 8192 67.4, 67.4, 65.4,
-// 108; 997 x 5003 20.5, 20.4, 17.0, 26.0; 4096 x 4096 33.3, 26.9, 27.4, 39.1; to 8 bits 4096 x 4096 13.6, 10.7, 10.6, 10.3).
+// from load to store), else four: more rows on a CU at a time (us, one, two, four, eight quads: to 8 bits 4096 x 4096 13.6, 10.7,
+// 10.6, 10.3, norms 4096 x 8192 67.4, 67.4, 68.0, 108; 997 x 5003 20.5, 20.4, 17.2, 26.0; 4096 x 4096 33.3, 26.9, 29.1, 39.1).
 // Rotated rows: four quads, eight where 16 waves do not hold the row so.
 struct Shape {
     int quads, waves, lds;
