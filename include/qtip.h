@@ -310,6 +310,7 @@ int qtip_quantize_ldlq(const float *W, const float *A, int m, int n, int L, int 
 
 #define QTIP_ROWS_MAX_N 32768 /* longest row of the calls that hold one in registers */
 #define QTIP_I8_MAX_N 131071  /* most inputs of an 8-bit product: n 128^2 stays below 2^31 */
+#define QTIP_I8_MAX_M (1 << 28)  /* most outputs of one */
 #define QTIP_I8_MAX_LD (1 << 24) /* most values between two rows of an 8-bit product's operands */
 #define QTIP_I8_MAX_B (65535 * 16)
 
@@ -336,7 +337,8 @@ int qtip_quantize_rows_i8(const void *x, const void *up, int type, int rows, int
  * The sum is exact (32-bit whole numbers); scales, bias and their sum are fp32, rounded once to y_type.
  *   W: m rows, X: B rows; both begin at multiples of 16 bytes (ldw and ldx are multiples of 16, so a row may be any n
  *   long; up to 15 bytes behind its end are read and count for nothing).  w_scale: m, x_scale: B, bias: m fp32 or NULL.
- *   Y: rows ldy apart, of y_type (F16, BF16, F32).  n at most QTIP_I8_MAX_N, B at most QTIP_I8_MAX_B.
+ *   Y: rows ldy apart, of y_type (F16, BF16, F32).  n at most QTIP_I8_MAX_N, m QTIP_I8_MAX_M, B QTIP_I8_MAX_B, ldw and
+ *   ldx QTIP_I8_MAX_LD.
  *   workspace: qtip_matmul_i8_workspace(m, n, B) bytes, 256-byte aligned; NULL where that is 0.  Contents are scratch.
  */
 size_t qtip_matmul_i8_workspace(int m, int n, int B);
@@ -374,11 +376,13 @@ int qtip_norm_residual(const void *y, int64_t ldy, int y_type, const void *h, in
  *     g = G_e x,  u = U_e x,  y = sum over the chosen e of p_e D_e (silu(g) .* u).
  * The experts' weights are 8-bit rows (as qtip_quantize_rows_i8 makes them), activations stay in 16 bits (the weights'
  * bytes are what a few tokens wait for); products, softmax and sums are fp32, y is rounded once.
- * Every chosen expert's weights are read once.
- *   x, y: T rows of n, ldx and ldy values apart, of `type` (F16, BF16); x 16-byte aligned, ldx a multiple of 8; y not x.
+ * A chosen expert's weights are read once for all tokens that chose it, up to 8 (for D) or 16 (for G and U) of them at a time,
+ * twice as many where an expert has many.
+ *   x, y: T rows of n, ldx and ldy values apart, of `type` (F16, BF16); x 16-byte aligned, ldx a multiple of 8
+ *   and at most QTIP_I8_MAX_LD; y not x.
  *   router: E x n of `type`.  router_bias: E fp32 or NULL; -infinity masks an expert.  A masked expert that is chosen for
- *   want of others has weight 0 and is left out; a token without any expert gets y = 0.  A NaN among a token's logits
- *   (a NaN in its x) makes all its weights NaN.
+ *   want of others has weight 0 and is left out; a token without any expert gets y = 0.  A NaN or +infinity among a
+ *   token's logits (from one in its x) makes all its weights NaN, and its y.
  *   W_up: E x 2f x n int8, an expert's rows of G, then those of U; up_scale: E x 2f fp32.  W_down: E x n x f int8;
  *   down_scale: E x n fp32.  n and f: multiples of 16, at most QTIP_ROWS_MAX_N.  All 16-byte aligned.
  *   ids: T x top_k int32, weights: T x top_k fp32, by descending l: the choice and p; either may be NULL.

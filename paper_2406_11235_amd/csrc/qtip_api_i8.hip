@@ -53,7 +53,7 @@ int qtip_quantize_rows_i8(const void *x, const void *up, int type, int rows, int
 }
 
 size_t qtip_matmul_i8_workspace(int m, int n, int B) {
-    if (m < 1 || n < 1 || n > QTIP_I8_MAX_N || B < 1 || B > QTIP_I8_MAX_B) return 0;
+    if (m < 1 || m > QTIP_I8_MAX_M || n < 1 || n > QTIP_I8_MAX_N || B < 1 || B > QTIP_I8_MAX_B) return 0;
     return qtip::matmul_i8_workspace(m, n, B);
 }
 
@@ -65,6 +65,7 @@ int qtip_matmul_i8(const int8_t *W, int64_t ldw, const float *w_scale, int m, in
     if (!is_float_type(y_type)) return fail(QTIP_EUNSUPPORTED, "%s: type %d is not F16, BF16 or F32", fn, y_type);
     if (m < 1 || n < 1) return fail(QTIP_EINVAL, "%s: m = %d and n = %d must be positive", fn, m, n);
     if (n > QTIP_I8_MAX_N) return fail(QTIP_EINVAL, "%s: n = %d is above QTIP_I8_MAX_N = %d", fn, n, QTIP_I8_MAX_N);
+    if (m > QTIP_I8_MAX_M) return fail(QTIP_EINVAL, "%s: m = %d is above QTIP_I8_MAX_M = %d", fn, m, QTIP_I8_MAX_M);
     if (B < 1 || B > QTIP_I8_MAX_B) return fail(QTIP_EINVAL, "%s: B = %d out of range", fn, B);
     if (int rc = check_matrix(fn, "W", W, ldw, n, QTIP_I8)) return rc;
     if (int rc = check_matrix(fn, "X", X, ldx, n, QTIP_I8)) return rc;

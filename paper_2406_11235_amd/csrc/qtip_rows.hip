@@ -270,7 +270,9 @@ __device__ __forceinline__ void normalize(float4_t (&v)[Q], int n, float over_n,
     for (int q = 0; q < Q; q++) v[q] *= scale;
 }
 
-template <class TY, class TH, int Q, bool ROT, bool RAGGED>
+// FEW: of few rows (the time from load to store counts, not how many are on a CU) everything is asked for at the beginning, weights
+// too (1 x 4096 rotated, in a graph, 4.95 us and 4.34 so).
+template <class TY, class TH, int Q, bool ROT, bool RAGGED, bool FEW>
 __global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a) {
     extern __shared__ float4_t s_v[];  // 1024 floats a wave where a row is rotated over waves
     __shared__ float s_sum[4][16];
@@ -282,7 +284,7 @@ __global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a) {
     typename Quad<TH>::type h[Q];
     // All of a row at once where that is few registers, else one matrix after the other, and more rows on a CU (us, at once and so:
     // 1024 x 28672 with an fp32 residual 116 and 92, 8192 x 1024 15.7 and 12.9, 997 x 5003 23.1 and 17.2, 4096 x 4096 27.4 and 29.1).
-    constexpr bool AT_ONCE = Q <= 2;
+    constexpr bool AT_ONCE = Q <= 2 || FEW;
     auto load_h = [&] {
         if (a.h) load_row<TH, Q, ROT, RAGGED>(h, (const TH *)a.h + row * a.ldh, n);
     };
@@ -297,10 +299,15 @@ __global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a) {
         load_h();
     }
     float4_t v[Q];
-    auto affine = [&](const float *weight, const float *bias) {
+    float4_t post[Q], pre[Q];
+    if constexpr (FEW) {
+        if (a.post) load_row<float, Q, ROT, RAGGED>(post, a.post, n);
+        if (a.pre) load_row<float, Q, ROT, RAGGED>(pre, a.pre, n);
+    }
+    auto affine = [&](const float4_t(&early)[Q], const float *weight, const float *bias) {
 #pragma unroll
         for (int q = 0; q < Q; q++) {
-            v[q] *= load_quad<RAGGED>(weight, quad_in<ROT>(q), n);
+            v[q] *= FEW ? early[q] : load_quad<RAGGED>(weight, quad_in<ROT>(q), n);
             if (bias) v[q] += load_quad<RAGGED>(bias, quad_in<ROT>(q), n);
         }
     };
@@ -308,7 +315,7 @@ __global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a) {
     for (int q = 0; q < Q; q++) v[q] = a.y ? widen(y[q]) : widen(h[q]);
     if (a.post) {
         normalize<Q, ROT>(v, n, over_n, a.layer, a.eps, s_sum, waves);
-        affine(a.post, a.post_bias);
+        affine(post, a.post, a.post_bias);
     }
     if constexpr (AT_ONCE) {
         if (a.y) {
@@ -339,7 +346,7 @@ __global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a) {
     if (!a.x) return;
     if (a.pre) {
         normalize<Q, ROT>(v, n, over_n, a.layer, a.eps, s_sum + 2, waves);
-        affine(a.pre, a.pre_bias);
+        affine(pre, a.pre, a.pre_bias);
     }
     Places o = {};
     if constexpr (ROT) o = rotate_row<Q>(v, a.signs, n, a.p, s_v);
@@ -407,8 +414,12 @@ hipError_t launch_quantize_rows_i8(const void *x, const void *up, int type, int 
 
 template <class TY, class TH> static void launch_norm(const NormResidual &a, int rows, hipStream_t st) {
     const Shape s = shape_of(rows, a.n, a.signs, a.p);
+    if (a.signs && rows <= CUS && a.n <= 8192) {
+        hipLaunchKernelGGL((norm_residual_kernel<TY, TH, 4, true, false, true>), dim3(rows), dim3(s.waves * 64), s.lds, st, a);
+        return;
+    }
 #define QTIP_NORM(Q, ROT, RAGGED) \
-    hipLaunchKernelGGL((norm_residual_kernel<TY, TH, Q, ROT, RAGGED>), dim3(rows), dim3(s.waves * 64), s.lds, st, a)
+    hipLaunchKernelGGL((norm_residual_kernel<TY, TH, Q, ROT, RAGGED, false>), dim3(rows), dim3(s.waves * 64), s.lds, st, a)
     QTIP_ROWS_BY_SHAPE(QTIP_NORM, s, a.n, a.signs);
 }
 

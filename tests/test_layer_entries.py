@@ -45,7 +45,7 @@ def test_quantize_rows_refuses(code, change):
 @pytest.mark.parametrize("code,change", [
     (EINVAL, dict(W=None)), (EINVAL, dict(X=None)), (EINVAL, dict(Y=None)), (EINVAL, dict(w_scale=None)), (EINVAL, dict(x_scale=None)),
     (EUNSUPPORTED, dict(y_type=q.I8)), (EINVAL, dict(m=0)), (EINVAL, dict(n=0)), (EINVAL, dict(B=0)), (EINVAL, dict(B=-1)),
-    (EINVAL, dict(n=131072, ldw=131072, ldx=131072)), (EINVAL, dict(B=65535 * 16 + 1)), (EINVAL, dict(ldw=(1 << 24) + 16)), (EINVAL, dict(ldx=(1 << 24) + 16)), (EINVAL, dict(ldw=48)), (EINVAL, dict(ldx=48)),
+    (EINVAL, dict(n=131072, ldw=131072, ldx=131072)), (EINVAL, dict(B=65535 * 16 + 1)), (EINVAL, dict(m=(1 << 28) + 1, ldy=1 << 29)), (EINVAL, dict(ldw=(1 << 24) + 16)), (EINVAL, dict(ldx=(1 << 24) + 16)), (EINVAL, dict(ldw=48)), (EINVAL, dict(ldx=48)),
     (EINVAL, dict(ldy=4)), (EINVAL, dict(ldw=72)), (EINVAL, dict(ldx=56)), (EINVAL, dict(W=P + 8)), (EINVAL, dict(X=P + 1)),
     (EINVAL, dict(Y=P + 2)), (EINVAL, dict(bias=P + 2)), (EINVAL, dict(w_scale=P + 1)), (EINVAL, dict(x_scale=P + 3))])
 def test_matmul_refuses(code, change):
@@ -84,7 +84,7 @@ def test_norm_residual_refuses(code, change):
     (EUNSUPPORTED, dict(type=q.F32)), (EINVAL, dict(T=0)), (EINVAL, dict(T=65)), (EINVAL, dict(E=0)), (EINVAL, dict(E=257)),
     (EINVAL, dict(top_k=0)), (EINVAL, dict(top_k=9)), (EINVAL, dict(top_k=17, E=64)), (EINVAL, dict(n=56)), (EINVAL, dict(f=24)),
     (EINVAL, dict(f=0)), (EINVAL, dict(n=0)), (EINVAL, dict(n=32784, ldx=32784, ldy=32784)), (EINVAL, dict(f=32784)),
-    (EINVAL, dict(ldx=56)), (EINVAL, dict(ldy=63)), (EINVAL, dict(ldx=68)), (EINVAL, dict(x=P + 8)), (EINVAL, dict(router=P + 8)),
+    (EINVAL, dict(ldx=56)), (EINVAL, dict(ldy=63)), (EINVAL, dict(ldx=68)), (EINVAL, dict(ldx=(1 << 24) + 8)), (EINVAL, dict(x=P + 8)), (EINVAL, dict(router=P + 8)),
     (EINVAL, dict(W_up=P + 4)), (EINVAL, dict(W_down=P + 4)), (EINVAL, dict(up_scale=P + 4)), (EINVAL, dict(down_scale=P + 8)),
     (EINVAL, dict(y=P + 1)), (EINVAL, dict(ids=P + 2)), (EINVAL, dict(weights=P + 2)), (EINVAL, dict(router_bias=P + 2)),
     (EINVAL, dict(workspace=P + 64)), (EINVAL, dict(workspace_bytes=q.qtip_moe_i8_workspace(2, 64, 32, 8, 2) - 1))])
