@@ -15,10 +15,13 @@ namespace qtip {
 
 namespace {
 
+// Whether and how rows are rotated: blocks of 1024 and more have all stages within a wave.
+enum Turn { NONE, SHORT_BLOCKS, LONG_BLOCKS };
+
 // Where a thread's quad number q lies in its row.  Rotated rows: a wave has 1024 neighbouring values (and, of rows above
 // 16384, 1024 more 16 waves on), a lane four quads of them 256 apart; which of 16 quads next to each other says rht_lane_t.
-template <bool ROT> __device__ __forceinline__ int quad_in(int q) {
-    if constexpr (ROT) {
+template <Turn ROT> __device__ __forceinline__ int quad_in(int q) {
+    if constexpr (ROT != NONE) {
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
         return 1024 * (wave + 16 * (q >> 2)) + 256 * (q & 3) + 64 * (lane >> 4) + 4 * rht_lane_t(lane & 15);
     } else {
@@ -29,9 +32,9 @@ template <bool ROT> __device__ __forceinline__ int quad_in(int q) {
 struct Places {
     int base, first, second;
 };
-template <bool ROT> __device__ __forceinline__ int quad_out(const Places &o, int q) {
-    if constexpr (ROT) return o.base + (q & 1 ? o.first : 0) + (q & 2 ? o.second : 0) + (q >> 2) * 16384;
-    else return quad_in<false>(q);
+template <Turn ROT> __device__ __forceinline__ int quad_out(const Places &o, int q) {
+    if constexpr (ROT != NONE) return o.base + (q & 1 ? o.first : 0) + (q & 2 ? o.second : 0) + (q >> 2) * 16384;
+    else return quad_in<NONE>(q);
 }
 
 // Four quads' butterflies over one bit of the quad's number.
@@ -72,18 +75,19 @@ template <bool WIDE> __device__ __forceinline__ void swap_stage(float4_t &a, flo
 // lanes of a row (basis 1, 2, 7, 15: rht_lane_t), 6-7 over rows of lanes, 8-9 over the lane's quads and the rest over waves: each
 // stage is between registers, through DPP, or between registers behind an exchange; two bits of the wave's number at a time change
 // places with the quad's through LDS.  Called by whole workgroups.  `half`: the four quads' number.  s_v: 1024 floats a wave.
-__device__ __forceinline__ Places rotate_quads(float4_t (&v)[4], int half, const int8_t *__restrict__ signs, int n, int p, float4_t *s_v) {
+template <Turn ROT> __device__ __forceinline__ Places rotate_quads(float4_t (&v)[4], int half, const int8_t *__restrict__ signs, int n, int p, float4_t *s_v) {
+    constexpr bool LONG = ROT == LONG_BLOCKS;  // (branches cost copies of registers: 2048 x 8192, blocks of 2048, 21.8 us and 17.3 so)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, t = rht_lane_t(lane & 15);
     uint32_t s[4];
 #pragma unroll
     for (int q = 0; q < 4; q++) {
-        const int at = quad_in<true>(4 * half + q);
+        const int at = quad_in<LONG_BLOCKS>(4 * half + q);
         s[q] = at < n ? *reinterpret_cast<const uint32_t *>(signs + at) : 0u;
     }
     const float s1 = t & 1 ? -1.f : 1.f, s2 = t & 2 ? -1.f : 1.f, s4 = t & 4 ? -1.f : 1.f, s8 = t & 8 ? -1.f : 1.f;
     float scale = rht_scale(p) * s1 * s2;
-    if (p > 4) scale *= s4;
-    if (p > 5) scale *= s8;
+    if (LONG || p > 4) scale *= s4;
+    if (LONG || p > 5) scale *= s8;
     float x[4][4];
 #pragma unroll
     for (int q = 0; q < 4; q++) {
@@ -96,30 +100,30 @@ __device__ __forceinline__ Places rotate_quads(float4_t (&v)[4], int half, const
         QTIP_LANE_STAGE(x[q], s1, "quad_perm:[1,0,3,2]");
         QTIP_LANE_STAGE(x[q], s2, "quad_perm:[2,3,0,1]");
     }
-    if (p > 4) {
+    if (LONG || p > 4) {
 #pragma unroll
         for (int q = 0; q < 4; q++) QTIP_LANE_STAGE(x[q], s4, "row_half_mirror");
     }
-    if (p > 5) {
+    if (LONG || p > 5) {
 #pragma unroll
         for (int q = 0; q < 4; q++) QTIP_LANE_STAGE(x[q], s8, "row_mirror");
     }
 #pragma unroll
     for (int q = 0; q < 4; q++) v[q] = float4_t{x[q][0], x[q][1], x[q][2], x[q][3]} * scale;
-    if (p > 8) {
+    if (LONG || p > 8) {
         quad_stage(v[0], v[1]);
         quad_stage(v[2], v[3]);
     }
-    if (p > 9) {
+    if (LONG || p > 9) {
         quad_stage(v[0], v[2]);
         quad_stage(v[1], v[3]);
     }
-    swap_stage<true>(v[0], v[1], p > 7);
-    swap_stage<true>(v[2], v[3], p > 7);
-    swap_stage<false>(v[0], v[2], p > 6);
-    swap_stage<false>(v[1], v[3], p > 6);
+    swap_stage<true>(v[0], v[1], LONG || p > 7);
+    swap_stage<true>(v[2], v[3], LONG || p > 7);
+    swap_stage<false>(v[0], v[2], LONG || p > 6);
+    swap_stage<false>(v[1], v[3], LONG || p > 6);
     const int base = 4 * t + 256 * (lane >> 5) + 512 * ((lane >> 4) & 1);
-    if (p <= 10) return Places{base + 1024 * wave, 128, 64};
+    if (!LONG || p == 10) return Places{base + 1024 * wave, 128, 64};
     // Quads against the waves of a group of two or four, which differ in the bits of their number from `low` on: this wave
     // takes the quads that have its own bits from each of them.
     auto exchange = [&](int low, bool four) {
@@ -148,13 +152,13 @@ __device__ __forceinline__ Places rotate_quads(float4_t (&v)[4], int half, const
     if (p == 13) return Places{quad + 2048 * (wave >> 2 & 1) + 1024 * (wave & ~7), 1024, 4096};
     return Places{quad + 1024 * (wave >> 2 & 3), 4096, 8192};
 }
-template <int Q>
+template <int Q, Turn ROT>
 __device__ __forceinline__ Places rotate_row(float4_t (&v)[Q], const int8_t *__restrict__ signs, int n, int p, float4_t *s_v) {
     Places o;
 #pragma unroll
     for (int c = 0; c < Q / 4; c++) {
         float4_t w[4] = {v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]};
-        o = rotate_quads(w, c, signs, n, p, s_v);
+        o = rotate_quads<ROT>(w, c, signs, n, p, s_v);
 #pragma unroll
         for (int q = 0; q < 4; q++) v[4 * c + q] = w[q];
     }
@@ -162,7 +166,7 @@ __device__ __forceinline__ Places rotate_row(float4_t (&v)[Q], const int8_t *__r
 }
 
 // The bits of the largest absolute value: they order as whole numbers, NaN above infinity, so one maximum finds those too.
-template <int Q, bool ROT> __device__ __forceinline__ uint32_t largest(const float4_t (&v)[Q], const Places &o, int n) {
+template <int Q, Turn ROT> __device__ __forceinline__ uint32_t largest(const float4_t (&v)[Q], const Places &o, int n) {
     uint32_t top = 0;
 #pragma unroll
     for (int q = 0; q < Q; q++)
@@ -177,7 +181,7 @@ template <int Q, bool ROT> __device__ __forceinline__ uint32_t largest(const flo
 }
 // v to 8 bits: scale = a / 127 and q = v (127 / a) to the nearest whole number, ties to even, a = `top` the row's largest absolute
 // value.  A row of zeros has the scale 0; one with an infinity or a NaN has the scale NaN, so that what is computed of it is NaN too.
-template <int Q, bool ROT, bool RAGGED>
+template <int Q, Turn ROT, bool RAGGED>
 __device__ __forceinline__ void store_i8(const float4_t (&v)[Q], const Places &o, int n, int8_t *__restrict__ to, float *scale, uint32_t top) {
     const float a = __builtin_bit_cast(float, top);
     const bool finite = top < 0x7F800000u;
@@ -208,7 +212,7 @@ __device__ __forceinline__ void store_i8(const float4_t (&v)[Q], const Places &o
     }
 }
 
-template <int Q, bool ROT, bool RAGGED>
+template <int Q, Turn ROT, bool RAGGED>
 __device__ __forceinline__ void store_row(const float4_t (&v)[Q], const Places &o, int n, int type, void *x, int64_t at_row) {
 #pragma unroll
     for (int q = 0; q < Q; q++) {
@@ -219,11 +223,11 @@ __device__ __forceinline__ void store_row(const float4_t (&v)[Q], const Places &
     }
 }
 
-template <class T, int Q, bool ROT, bool RAGGED> __device__ __forceinline__ void load_row(typename Quad<T>::type (&v)[Q], const T *row, int n) {
+template <class T, int Q, Turn ROT, bool RAGGED> __device__ __forceinline__ void load_row(typename Quad<T>::type (&v)[Q], const T *row, int n) {
 #pragma unroll
     for (int q = 0; q < Q; q++) v[q] = load_quad<RAGGED>(row, quad_in<ROT>(q), n);
 }
-template <class T, int Q, bool ROT, bool RAGGED>
+template <class T, int Q, Turn ROT, bool RAGGED>
 __global__ __launch_bounds__(1024) void quantize_rows_kernel(const T *__restrict__ x, const T *__restrict__ up, int n, int64_t ldx,
                                                              const int8_t *__restrict__ signs, int p, int8_t *__restrict__ out,
                                                              int64_t ldq, float *__restrict__ scale) {
@@ -244,13 +248,13 @@ __global__ __launch_bounds__(1024) void quantize_rows_kernel(const T *__restrict
         }
     }
     Places o = {};
-    if constexpr (ROT) o = rotate_row<Q>(v, signs, n, p, s_v);
+    if constexpr (ROT != NONE) o = rotate_row<Q, ROT>(v, signs, n, p, s_v);
     const uint32_t top = block_max(largest<Q, ROT>(v, o, n), s_max, blockDim.x >> 6);
     store_i8<Q, ROT, RAGGED>(v, o, n, out + row * ldq, scale + row, top);
 }
 
 // v: (v - mean) / sqrt(mean of (v - mean)^2 + eps) * weight + bias; the mean is 0 where the norm has none.  Zeros beyond n stay.
-template <int Q, bool ROT>
+template <int Q, Turn ROT>
 __device__ __forceinline__ void normalize(float4_t (&v)[Q], int n, float over_n, bool layer, float eps, float (*slots)[16], int waves) {
     if (layer) {
         float t = 0.f;
@@ -272,7 +276,7 @@ __device__ __forceinline__ void normalize(float4_t (&v)[Q], int n, float over_n,
 
 // FEW: of few rows (the time from load to store counts, not how many are on a CU) everything is asked for at the beginning, weights
 // too (1 x 4096 rotated, in a graph, 4.95 us and 4.34 so).
-template <class TY, class TH, int Q, bool ROT, bool RAGGED, bool FEW>
+template <class TY, class TH, int Q, Turn ROT, bool RAGGED, bool FEW>
 __global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a) {
     extern __shared__ float4_t s_v[];  // 1024 floats a wave where a row is rotated over waves
     __shared__ float s_sum[4][16];
@@ -349,7 +353,7 @@ __global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a) {
         affine(pre, a.pre, a.pre_bias);
     }
     Places o = {};
-    if constexpr (ROT) o = rotate_row<Q>(v, a.signs, n, a.p, s_v);
+    if constexpr (ROT != NONE) o = rotate_row<Q, ROT>(v, a.signs, n, a.p, s_v);
     if (a.x_type == TYPE_I8) {
         const uint32_t top = block_max(largest<Q, ROT>(v, o, n), s_max, waves);
         store_i8<Q, ROT, RAGGED>(v, o, n, (int8_t *)a.x + row * a.ldx, a.x_scale + row, top);
@@ -373,8 +377,8 @@ int log2_of(int block) {
 struct Shape {
     int quads, waves, lds;
 };
-static Shape shape_of(int rows, int n, bool rot, int p) {
-    if (rot) {
+static Shape shape_of(int rows, int n, int p) {
+    if (p) {
         const int waves = n <= 16384 ? (n + 1023) / 1024 : 16;
         return {n <= 16384 ? 4 : 8, waves, p > 10 ? waves * 4096 : 0};
     }
@@ -387,20 +391,22 @@ static Shape shape_of(int rows, int n, bool rot, int p) {
     else if (s.quads == 2) LAUNCH(2, rot, ragged);  \
     else if (s.quads == 4) LAUNCH(4, rot, ragged);  \
     else LAUNCH(8, rot, ragged)
-#define QTIP_ROWS_BY_SHAPE(LAUNCH, s, n, rot)                         \
-    if (rot && s.quads == 4) { LAUNCH(4, true, false); }              \
-    else if (rot) { LAUNCH(8, true, false); }                         \
-    else if (n % 4) { QTIP_ROWS_BY_QUADS(LAUNCH, s, false, true); }   \
-    else { QTIP_ROWS_BY_QUADS(LAUNCH, s, false, false); }
+#define QTIP_ROWS_BY_SHAPE(LAUNCH, s, n, p)                               \
+    if (p >= 10 && s.quads == 4) { LAUNCH(4, LONG_BLOCKS, false); }       \
+    else if (p >= 10) { LAUNCH(8, LONG_BLOCKS, false); }                  \
+    else if (p && s.quads == 4) { LAUNCH(4, SHORT_BLOCKS, false); }       \
+    else if (p) { LAUNCH(8, SHORT_BLOCKS, false); }                       \
+    else if (n % 4) { QTIP_ROWS_BY_QUADS(LAUNCH, s, NONE, true); }        \
+    else { QTIP_ROWS_BY_QUADS(LAUNCH, s, NONE, false); }
 
 template <class T>
 static void launch_quantize(const void *x, const void *up, int rows, int n, int64_t ldx, const int8_t *signs, int p, int8_t *q,
                             int64_t ldq, float *scale, hipStream_t st) {
-    const Shape s = shape_of(rows, n, signs, p);
+    const Shape s = shape_of(rows, n, p);
 #define QTIP_QUANTIZE(Q, ROT, RAGGED)                                                                                                 \
     hipLaunchKernelGGL((quantize_rows_kernel<T, Q, ROT, RAGGED>), dim3(rows), dim3(s.waves * 64), s.lds, st, (const T *)x, (const T *)up, n, \
                        ldx, signs, p, q, ldq, scale)
-    QTIP_ROWS_BY_SHAPE(QTIP_QUANTIZE, s, n, signs);
+    QTIP_ROWS_BY_SHAPE(QTIP_QUANTIZE, s, n, p);
 }
 
 hipError_t launch_quantize_rows_i8(const void *x, const void *up, int type, int rows, int n, int64_t ldx, const int8_t *signs,
@@ -413,14 +419,15 @@ hipError_t launch_quantize_rows_i8(const void *x, const void *up, int type, int 
 }
 
 template <class TY, class TH> static void launch_norm(const NormResidual &a, int rows, hipStream_t st) {
-    const Shape s = shape_of(rows, a.n, a.signs, a.p);
-    if (a.signs && rows <= CUS && a.n <= 8192) {
-        hipLaunchKernelGGL((norm_residual_kernel<TY, TH, 4, true, false, true>), dim3(rows), dim3(s.waves * 64), s.lds, st, a);
+    const Shape s = shape_of(rows, a.n, a.p);
+    if (a.p && rows <= CUS && a.n <= 8192) {
+        if (a.p >= 10) hipLaunchKernelGGL((norm_residual_kernel<TY, TH, 4, LONG_BLOCKS, false, true>), dim3(rows), dim3(s.waves * 64), s.lds, st, a);
+        else hipLaunchKernelGGL((norm_residual_kernel<TY, TH, 4, SHORT_BLOCKS, false, true>), dim3(rows), dim3(s.waves * 64), s.lds, st, a);
         return;
     }
 #define QTIP_NORM(Q, ROT, RAGGED) \
     hipLaunchKernelGGL((norm_residual_kernel<TY, TH, Q, ROT, RAGGED, false>), dim3(rows), dim3(s.waves * 64), s.lds, st, a)
-    QTIP_ROWS_BY_SHAPE(QTIP_NORM, s, a.n, a.signs);
+    QTIP_ROWS_BY_SHAPE(QTIP_NORM, s, a.n, a.p);
 }
 
 hipError_t launch_norm_residual(NormResidual a, int y_type, int h_type, int rows, int block, hipStream_t st) {
