@@ -253,16 +253,54 @@ __global__ __launch_bounds__(WM *WN * 64) void matmul_i8_tile_kernel(MatmulI8 a,
         half(std::integral_constant<int, 1>{}, next, s + 1 < stages, s + RING, slot, s + RING < stages);
         slot = next;
     }
+    if (sums) {
+#pragma unroll
+        for (int c = 0; c < RB; c++) {
+            const int b = b0 + (wn * RB + c) * 16 + (lane & 15);
+#pragma unroll
+            for (int r = 0; r < RA; r++) {
+                const int i = i0 + (wm * RA + r) * 16 + 4 * hi;
+                if (b < a.B && i < a.m) *reinterpret_cast<i32x4_t *>(sums + ((int64_t)part * a.B + b) * ((a.m + 3) & ~3) + i) = sum[r][c];
+            }
+        }
+        return;
+    }
+    // Sixteen batch rows at a time through a part of LDS that is the wave's own, so that a row's outputs go out as 16 bytes a lane
+    // and not as a lane's four (bf16, 28672 x 64, 4096 rows: 134.3 us as four, 71.9 so; 14336 x 4096, 997 rows: 63.6 and 54.4).
+    // (no copy is under way any more, and after the barrier nobody reads a stage)
+    constexpr int COLS = 16 * RA, PITCH = COLS * (int)sizeof(T) + 16, EACH = 16 / (int)sizeof(T), UNITS = COLS / EACH;
+    static_assert(NW * 16 * PITCH <= RING * STAGE, "room for sixteen rows of each wave");
+    char *const rows = s_tile + wave * 16 * PITCH;
+    const int i_wave = i0 + wm * COLS;
+    float4_t scale[RA], bias[RA];
+#pragma unroll
+    for (int r = 0; r < RA; r++) {
+        scale[r] = load_quad(a.w_scale, i_wave + 16 * r + 4 * hi, a.m);
+        bias[r] = a.bias ? load_quad(a.bias, i_wave + 16 * r + 4 * hi, a.m) : float4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    __syncthreads();
 #pragma unroll
     for (int c = 0; c < RB; c++) {
-        const int b = b0 + (wn * RB + c) * 16 + (lane & 15);
-        if (b >= a.B) continue;
+        const int b_first = b0 + (wn * RB + c) * 16;
+        const float xs = b_first + (lane & 15) < a.B ? a.x_scale[b_first + (lane & 15)] : 0.f;
 #pragma unroll
         for (int r = 0; r < RA; r++) {
-            const int i = i0 + (wm * RA + r) * 16 + 4 * hi;
-            if (i >= a.m) continue;
-            if (sums) *reinterpret_cast<i32x4_t *>(sums + ((int64_t)part * a.B + b) * ((a.m + 3) & ~3) + i) = sum[r][c];
-            else store_outputs<T>(a, b, i, sum[r][c]);
+            const float4_t v = __builtin_convertvector(sum[r][c], float4_t) * (scale[r] * xs) + bias[r];
+            *reinterpret_cast<typename Quad<T>::type *>(rows + (lane & 15) * PITCH + (16 * r + 4 * hi) * (int)sizeof(T)) =
+                __builtin_convertvector(v, typename Quad<T>::type);
+        }
+        typedef uint32_t anywhere __attribute__((ext_vector_type(4), aligned(2)));
+#pragma unroll
+        for (int u = lane; u < 16 * UNITS; u += 64) {
+            const int b = b_first + u / UNITS, i = i_wave + u % UNITS * EACH;
+            const char *from = rows + u / UNITS * PITCH + u % UNITS * 16;
+            if (b >= a.B || i >= a.m) continue;
+            T *to = (T *)a.Y + (int64_t)b * a.ldy + i;
+            if (i + EACH <= a.m) {
+                *reinterpret_cast<anywhere *>(to) = *reinterpret_cast<const u32x4_t *>(from);
+            } else {
+                for (int e = 0; i + e < a.m; e++) to[e] = reinterpret_cast<const T *>(from)[e];
+            }
         }
     }
 }
