@@ -305,13 +305,19 @@ __global__ __launch_bounds__(WM *WN * 64) void matmul_i8_tile_kernel(MatmulI8 a,
     }
 }
 
-// The parts' sums.
+// The parts' sums, eight loads under way at a time (64 x 28672, 100 rows, sixteen parts: 13.4 us one load after the other, 10.8 so).
 template <class T> __global__ __launch_bounds__(256) void matmul_i8_join_kernel(MatmulI8 a, int parts, const int32_t *__restrict__ sums) {
     const int i = 4 * (blockIdx.x * 256 + threadIdx.x), b = blockIdx.y;
     if (i >= a.m) return;
     const int64_t wide = (a.m + 3) & ~3;
     i32x4_t t = {0, 0, 0, 0};
-    for (int p = 0; p < parts; p++) t += *reinterpret_cast<const i32x4_t *>(sums + ((int64_t)p * a.B + b) * wide + i);
+    for (int p = 0; p < parts; p += 8) {
+        i32x4_t v[8];
+#pragma unroll
+        for (int d = 0; d < 8; d++) v[d] = *reinterpret_cast<const i32x4_t *>(sums + ((int64_t)min(p + d, parts - 1) * a.B + b) * wide + i);
+#pragma unroll
+        for (int d = 0; d < 8; d++) t += p + d < parts ? v[d] : i32x4_t{0, 0, 0, 0};
+    }
     store_outputs<T>(a, b, i, t);
 }
 
