@@ -36,7 +36,8 @@ __device__ __forceinline__ void store_outputs(const MatmulI8 &a, int b, int i, i
 // 16 MR outputs x 8 XC batch rows by a workgroup; its waves take 128 inputs in turn and add up at the end.  Each wave has a
 // ring of D stages in LDS to itself, filled by copies past the registers, eight whole rows of 128 bytes each: so many
 // bytes can be under way at a time, and no wave waits for another before the end.  Unit c (16 bytes) of row r is at place
-// c ^ (r / 2 % 8): 16 rows one after the other have the same unit in different banks.
+// c ^ (r / 2 % 8): 16 rows one after the other have the same unit in different banks.  Bound by reading the weights: 8192 x 28672,
+// 16 rows, 42.8 us, 5.5 TB/s (weights straight into registers, 62); by the launch at 4096 x 4096, 1 row, 4.7 us.
 template <class T, int MR, int XC, int NW, int D>
 __global__ __launch_bounds__(NW * 64) void matmul_i8_few_kernel(MatmulI8 a) {
     constexpr int NB = (XC + 1) / 2, WC = 2 * MR, STAGE = (WC + 2 * NB) * 1024;
@@ -136,7 +137,10 @@ __global__ __launch_bounds__(NW * 64) void matmul_i8_few_kernel(MatmulI8 a) {
 constexpr int STAGE_K = 128;
 
 // BM outputs x BN batch rows by a workgroup of WM x WN waves, RA x RB blocks of 16 x 16 each: weights are the rows of the matrix
-// instruction's result, batch rows its columns.  Both come into LDS by copies past the registers, a stage ahead.
+// instruction's result, batch rows its columns.  Both come into LDS by copies past the registers, a stage ahead.  Bound by the matrix
+// cores and by LDS, which one 256 x 256 tile keeps about equally busy, in turn with what a CU may draw: 8192 x 28672, 4096 rows, 714 us,
+// 2.7 * 10^15 operations a second, where the instructions alone, on registers of random bytes, reach 4.1 * 10^15 (without the copies
+// the loop takes 582 us, without its products' reads of LDS 701, with its copies alone 642).
 template <class T, int WM, int WN, int RA, int RB, int RING>
 __global__ __launch_bounds__(WM *WN * 64) void matmul_i8_tile_kernel(MatmulI8 a, int tiles_m, int tiles_b, int parts, int32_t *sums) {
     constexpr int NW = WM * WN, BM = 16 * RA * WM, BN = 16 * RB * WN, STAGE = (BM + BN) * STAGE_K;
@@ -328,9 +332,9 @@ struct Cut {
 };
 // What a stage takes (us) while a CU has one workgroup and while it has two, with enough tiles for that on all CUs:
 // 256 x 256 with two stages in LDS, 128 x 128 with two (two workgroups on a CU) and with three (one), 128 x 64 with three.
-// Measured: 8192 x 28672, 4096 rows 736 us with 256 x 256; 8192 x 8192: 1024 rows 68.8 with 128 x 128 and two stages (94.9 with
-// 256 x 256), 512 rows 41.9 with three stages (51.7 with two), 256 rows 30.0 with 128 x 64 (37.5); 14336 x 4096: 997 rows 62.1
-// with 256 x 256 (69.9 with 128 x 128), 512 rows 37.2 with 128 x 128, 256 rows 24.9 with it (26.0 with 128 x 64).
+// Measured (us, bf16, each tile in as many parts as suit it): 8192 x 28672, 4096 rows 719, 956, 1030, 1261; 14336 x 4096, 997 rows
+// 57.0, 69.5, 79.3, 81.7; 8192 x 8192, 1024 rows 82.0, 66.7, 78.9, 89.4; 14336 x 4096, 512 rows 54.9, 35.1, 42.0, 44.4; 8192 x 8192,
+// 512 rows 58.6, 48.6, 40.9, 45.4, 256 rows 42.8, 39.5, 30.3, 28.3, 128 rows 32.4, 26.1, 22.3, 21.5.
 constexpr int TILE_M[4] = {256, 128, 128, 128}, TILE_B[4] = {256, 128, 128, 64};
 constexpr float STAGE_ONE[4] = {1.64f, 0.8f, 0.65f, 0.465f}, STAGE_TWO[4] = {3.28f, 1.08f, 1.3f, 0.73f};
 
@@ -349,7 +353,8 @@ Cut cut_of(int m, int n, int B) {
             const int64_t work = tiles * parts, rest = work % (2 * CUS);
             float cost = (float)(work / (2 * CUS)) * STAGE_TWO[tile] + (rest == 0 ? 0.f : rest <= CUS ? STAGE_ONE[tile] : STAGE_TWO[tile]);
             cost *= (float)((stages + parts - 1) / parts);
-            // a launch, and the sums written and read: 8192 x 8192, 128 rows, 25.7 us in one part, 20.1 in two
+            // a launch, and the sums written and read: 8192 x 8192, 128 rows, 25.5 us in one part, 22.8 in two; 4096 x 4096, 64 rows,
+            // 14.5 in one, 10.7 so; 4096 x 28672, 100 rows, 105 and 34.8
             if (parts > 1) cost += 2.5f + 1.6e-6f * (float)parts * (float)m * (float)B;
             if (least == 0.f || cost < least) {
                 least = cost;
