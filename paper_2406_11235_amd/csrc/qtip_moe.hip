@@ -7,6 +7,9 @@
 // sums.  The products run on the matrix cores with 16 rows of weights as one operand and 16 rows of activations as the other;
 // weights become 16-bit floats on the way, exactly.  h lives in memory as the sum of two bf16 numbers (16 bits of mantissa at
 // any size), two rows of activations for D, so that y is what binary32 would give before its one rounding.
+// Measured: 1 token, 2 of 8 experts of 14336 x 4096, 353 MB, 78 us: 50 for G and U (4.7 TB/s), 22 for D (5.3), the rest launches, logits
+// and the choice; 64 tokens, 4 of 32 experts of 2048 x 4096, 805 MB, 180 us: 104 (5.2) and 62 (4.3: two rows for an h, so that some
+// experts have more than 16), logits, choice and sums 14.
 #include <type_traits>
 
 #include "qtip_copy_device.h"
