@@ -12,7 +12,11 @@ namespace {
 
 typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int FEW_ROWS = 32;  // batch rows that are taken at once, weights read once
+// Whether all batch rows are taken at once, and no more than once each weight: to 16, and to 32 unless one workgroup's inputs are so
+// many and the workgroups so few that parts of the inputs are worth a second launch (bf16, us, at once and in parts, 32 rows:
+// 64 x 16384 7.7 and 8.5, 64 x 28672 15.3 and 10.4, 1024 x 16384 10.3 and 9.8, 1024 x 28672 16.7 and 11.9, 4096 x 28672 30.5 and 26.9;
+// 24 rows: 1024 x 28672 15.3 and 11.8; 16 rows: 64 x 28672 8.5 and 10.3, 2048 x 28672 13.4 and 14.6).
+bool few_rows(int m, int n, int B) { return B <= 16 || (B <= 32 && (n <= 16384 || m >= 8192)); }
 
 // The first `count` of 16 bytes, zeros behind them.
 __device__ __forceinline__ i32x4_t keep_bytes(i32x4_t v, int count) {
@@ -325,7 +329,7 @@ template <class T> __global__ __launch_bounds__(256) void matmul_i8_join_kernel(
     store_outputs<T>(a, b, i, t);
 }
 
-// How the product of more than 32 rows is cut: the tile, how many stages of it LDS holds, and into how many parts the
+// How the product of rows that are not few is cut: the tile, how many stages of it LDS holds, and into how many parts the
 // inputs are. Where tiles leave CUs idle, a smaller tile or parts in the inputs fill them.
 struct Cut {
     int tile, parts;
@@ -369,7 +373,7 @@ template <class T, int MR, int XC, int NW, int D> hipError_t launch_few(const Ma
     hipLaunchKernelGGL((matmul_i8_few_kernel<T, MR, XC, NW, D>), dim3((a.m + 16 * MR - 1) / (16 * MR)), dim3(NW * 64), 0, st, a);
     return hipGetLastError();
 }
-// Up to 32 rows: each weight is read once and all rows at once, and what counts is how many bytes are under way.  Many outputs:
+// Few rows: each weight is read once and all rows at once, and what counts is how many bytes are under way.  Many outputs:
 // several 16s of them a workgroup share the copies of X; few: one, with as many waves as there are stages for.
 // (us; 2 x 16 outputs, 1 x 16 by 16 waves, by 8: 8192 x 28672, 16 rows, 43.5, 46.6, 47.3; 28672 x 4096, 1 row, 25.8, 27.2, 24.8;
 // 4096 x 4096, 1 row, 5.3, 4.8, 5.8; 4096 x 28672, 16 rows, 32.1, 24.5, 25.1; 28672 x 1024, 8 rows, 9.9, 13.1, 8.5.  4 x 16 and 1 x 16
@@ -398,7 +402,7 @@ hipError_t launch_tiles(const MatmulI8 &a, int parts, int32_t *sums, hipStream_t
 template <class T> hipError_t launch(const MatmulI8 &a, int32_t *sums, hipStream_t st) {
     if (a.B <= 8) return launch_few_rows<T, 1>(a, st);
     if (a.B <= 16) return launch_few_rows<T, 2>(a, st);
-    if (a.B <= FEW_ROWS) return launch_few_rows<T, 4>(a, st);
+    if (few_rows(a.m, a.n, a.B)) return launch_few_rows<T, 4>(a, st);
     const Cut cut = cut_of(a.m, a.n, a.B);
     if (cut.tile == 0) return launch_tiles<T, 0, 2, 4, 8, 4, 2>(a, cut.parts, sums, st);
     if (cut.tile == 1) return launch_tiles<T, 1, 4, 2, 2, 4, 2>(a, cut.parts, sums, st);
@@ -409,7 +413,7 @@ template <class T> hipError_t launch(const MatmulI8 &a, int32_t *sums, hipStream
 }  // namespace
 
 size_t matmul_i8_workspace(int m, int n, int B) {
-    if (B <= FEW_ROWS) return 0;
+    if (few_rows(m, n, B)) return 0;
     const Cut cut = cut_of(m, n, B);
     return cut.parts > 1 ? (size_t)cut.parts * B * (((size_t)m + 3) & ~(size_t)3) * 4 : 0;
 }

@@ -88,6 +88,14 @@ def test_every_count_of_rows(q, B):
     check(q, 300, 1000, B, "f16")
 
 
+@pytest.mark.parametrize("m,n", [(1, 16400), (64, 28672), (300, 16385), (4099, 16391), (8200, 17000)])
+@pytest.mark.parametrize("B", [16, 17, 31, 32])
+def test_long_rows_of_few_outputs(q, m, n, B):
+    """Parts of the inputs below 33 rows."""
+    check(q, m, n, B, "bf16", True)
+    check(q, m, n, B, "f32", False, "uniform", 16, 32, 1, 3)
+
+
 @pytest.mark.parametrize("m,n,B", [(64, 131071, 3), (64, 131071, 40), (300, 131056, 300), (1, 100000, 1)])
 @pytest.mark.parametrize("values", ["largest", "uniform"])
 def test_longest_rows_of_the_largest_values(q, m, n, B, values):
