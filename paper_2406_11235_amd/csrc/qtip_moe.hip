@@ -9,7 +9,7 @@
 // any size), two rows of activations for D, so that y is what binary32 would give before its one rounding.
 // Measured: 1 token, 2 of 8 experts of 14336 x 4096, 353 MB, 78 us: 50 for G and U (4.7 TB/s), 22 for D (5.3), the rest launches, logits
 // and the choice; 64 tokens, 4 of 32 experts of 2048 x 4096, 805 MB, 180 us: 104 (5.2) and 62 (4.3: two rows for an h, so that some
-// experts have more than 16), logits, choice and sums 14.
+// experts have more than 16), logits, choice and sums 11.
 #include <type_traits>
 
 #include "qtip_copy_device.h"
@@ -95,7 +95,7 @@ template <class T> __global__ __launch_bounds__(256) void moe_logits_kernel(MoeI
     }
 }
 
-// The choice by a workgroup of WAVES waves, which take tokens in turn.  plan is left whole; what goes to memory is written where
+// The choice by a workgroup of WAVES waves, which take tokens in turn, PER experts a lane.  plan is left whole; what goes to memory is written where
 // `write` says so.  (Loops are kept as loops: the code runs once, and fetching it is much of the time that takes: 16 tokens, 64 experts
 // of 1024 x 2048, the whole layer, 80.8 us with the loop over tokens unrolled, 76.4 so.)
 struct ChoiceLds {
@@ -105,8 +105,7 @@ struct ChoiceLds {
     int id[MOE_MAX_TOKENS * MOE_MAX_TOP_K];
     float weight[MOE_MAX_TOKENS * MOE_MAX_TOP_K];
 };
-template <int WAVES> __device__ __forceinline__ void choose(const MoeI8 &a, const Workspace &ws, ChoiceLds &s, bool write) {
-    constexpr int PER = MOE_MAX_EXPERTS / 64;  // experts of a lane
+template <int WAVES, int PER> __device__ __forceinline__ void choose(const MoeI8 &a, const Workspace &ws, ChoiceLds &s, bool write) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     for (int e = threadIdx.x; e < a.E; e += WAVES * 64) s.tokens[e] = 0;
     __syncthreads();
@@ -155,8 +154,9 @@ template <int WAVES> __device__ __forceinline__ void choose(const MoeI8 &a, cons
             chosen += w;
             id = lane == j ? found : id;
             mine = lane == j ? w : mine;
-            high = max(max(key[0], key[1]), max(key[2], key[3]));
-            static_assert(PER == 4, "of four keys");
+            high = key[0];
+#pragma unroll
+            for (int i = 1; i < PER; i++) high = max(high, key[i]);
             high = wave_max(high);
         }
         const float sum = a.renormalize ? chosen : wave_sum(all);
@@ -212,9 +212,9 @@ template <int WAVES> __device__ __forceinline__ void choose(const MoeI8 &a, cons
         ws.choices[c] = Choice{weight, weight == 0.f ? -1 : s.first[id] + __builtin_popcountll(s.tokens[id] & before)};
     }
 }
-__global__ __launch_bounds__(1024) void moe_choose_kernel(MoeI8 a, Workspace ws) {
+template <int PER> __global__ __launch_bounds__(1024) void moe_choose_kernel(MoeI8 a, Workspace ws) {
     __shared__ ChoiceLds s;
-    choose<16>(a, ws, s, true);
+    choose<16, PER>(a, ws, s, true);
 }
 
 // Sixteen weights as two operands of eight, in the activations' type.
@@ -381,23 +381,23 @@ __device__ __forceinline__ int bit_of(uint64_t bits, int r) {
     return __builtin_ctzll(bits);
 }
 
-// h of 16 rows of G and U of one expert.  CHOOSE: for as many tokens as there are waves, every workgroup makes the choice
+// h of 16 rows of G and U of one expert.  CHOOSE, experts a lane of the choice: for as many tokens as there are waves, every workgroup makes the choice
 // itself, which takes less than a launch (1 token, 2 of 8 experts of 14336 x 4096: 78.3 us, with a launch 79.9), and the first
 // one writes it down.
-template <class T, bool CHOOSE, bool WIDE> __global__ __launch_bounds__(NW * 64, WGS<WIDE>) void moe_up_kernel(MoeI8 a, Workspace ws) {
+template <class T, int CHOOSE, bool WIDE> __global__ __launch_bounds__(NW * 64, WGS<WIDE>) void moe_up_kernel(MoeI8 a, Workspace ws) {
     __shared__ __attribute__((aligned(1024))) char s_ring[NW * WAVE_LDS<WIDE>];
     const int u = blockIdx.y;
     const Plan *plan = ws.plan;
-    if constexpr (CHOOSE) {
+    if constexpr (CHOOSE > 0) {
         ChoiceLds &s = *reinterpret_cast<ChoiceLds *>(s_ring);
-        choose<NW>(a, ws, s, blockIdx.x == 0 && u == 0);
+        choose<NW, CHOOSE>(a, ws, s, blockIdx.x == 0 && u == 0);
         plan = &s.plan;
     }
     if (u >= plan->experts) return;
     const int e = plan->expert[u], first = plan->first[u];
     const uint64_t tokens = plan->tokens[u];
     const int count = __builtin_popcountll(tokens);
-    if constexpr (CHOOSE) __syncthreads();  // (the ring is where the choice was made)
+    if constexpr (CHOOSE > 0) __syncthreads();  // (the ring is where the choice was made)
     const int i0 = blockIdx.x * 16, i = i0 + 4 * ((threadIdx.x & 63) >> 4);
     const u32x4_t buffer_w = buffer_of(a.W_up + (int64_t)e * 2 * a.f * a.n, (size_t)2 * a.f * a.n);
     const u32x4_t buffer_x = buffer_of(a.x, ((size_t)(a.T - 1) * a.ldx + a.n) * 2);
@@ -463,15 +463,20 @@ template <class T> __global__ __launch_bounds__(256) void moe_join_kernel(MoeI8 
     store_quad((T *)a.y + t * a.ldy, i, a.n, y);
 }
 
+// Experts a lane has in the choice: one where that is enough (the choice's kernel: 64 tokens, 4 of 32 experts, 7.4 us, with four
+// for all 10.6; 16 tokens, 8 of 64, 4.7 and 5.8).
+constexpr int MOST = MOE_MAX_EXPERTS / 64;
 template <class T> void launch_moe(const MoeI8 &a, const Workspace &ws, hipStream_t st) {
     hipLaunchKernelGGL((moe_logits_kernel<T>), dim3(a.E, (a.T + 3) / 4), dim3(256), 0, st, a, ws.logits);
     const int experts = a.T * a.top_k < a.E ? a.T * a.top_k : a.E;
     if (a.T <= NW) {
-        hipLaunchKernelGGL((moe_up_kernel<T, true, false>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
+        if (a.E <= 64) hipLaunchKernelGGL((moe_up_kernel<T, 1, false>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
+        else hipLaunchKernelGGL((moe_up_kernel<T, MOST, false>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
     } else {
-        hipLaunchKernelGGL(moe_choose_kernel, dim3(1), dim3(1024), 0, st, a, ws);
-        if (wide(a)) hipLaunchKernelGGL((moe_up_kernel<T, false, true>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
-        else hipLaunchKernelGGL((moe_up_kernel<T, false, false>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
+        if (a.E <= 64) hipLaunchKernelGGL((moe_choose_kernel<1>), dim3(1), dim3(1024), 0, st, a, ws);
+        else hipLaunchKernelGGL((moe_choose_kernel<MOST>), dim3(1), dim3(1024), 0, st, a, ws);
+        if (wide(a)) hipLaunchKernelGGL((moe_up_kernel<T, 0, true>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
+        else hipLaunchKernelGGL((moe_up_kernel<T, 0, false>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
     }
     if (wide(a)) hipLaunchKernelGGL((moe_down_kernel<true>), dim3((a.n + 31) / 32, experts), dim3(NW * 64), 0, st, a, ws);
     else hipLaunchKernelGGL((moe_down_kernel<false>), dim3((a.n + 31) / 32, experts), dim3(NW * 64), 0, st, a, ws);
