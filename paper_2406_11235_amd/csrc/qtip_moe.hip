@@ -8,8 +8,8 @@
 // weights become 16-bit floats on the way, exactly.  h lives in memory as the sum of two bf16 numbers (16 bits of mantissa at
 // any size), two rows of activations for D, so that y is what binary32 would give before its one rounding.
 // Measured: 1 token, 2 of 8 experts of 14336 x 4096, 353 MB, 78 us: 50 for G and U (4.7 TB/s), 22 for D (5.3), the rest launches, logits
-// and the choice; 64 tokens, 4 of 32 experts of 2048 x 4096, 805 MB, 180 us: 104 (5.2) and 62 (4.3: two rows for an h, so that some
-// experts have more than 16), logits, choice and sums 11.
+// and the choice; 64 tokens, 4 of 32 experts of 2048 x 4096, 805 MB, 176 us: 104 (5.2) and 58 (4.6),
+// logits, choice and sums 11.
 #include <type_traits>
 
 #include "qtip_copy_device.h"
@@ -244,10 +244,11 @@ __device__ __forceinline__ void weights_of(i32x4_t v, typename Operand<T>::type 
 }
 
 // The waves of a workgroup, the LDS that each has to itself, and workgroups on a CU: 10 KiB and four, so that the work of one fills
-// the others' beginnings and ends (16 tokens, 64 experts of 1024 x 2048: 79 us, with 20 KiB and two 90), and 16 rows of
-// activations at a time.  WIDE, 20 KiB and two: 32 rows at a time, where an expert has many tokens and 16 rows would have its weights
-// read more often (64 tokens, us, narrow and wide: 2 of 8 experts of 14336 x 4096 443 and 364, 4 of 16 of 2048 x 4096 150 and 133,
-// 4 of 32 185 and 195; 32 tokens, 4 of 16 104 and 109).
+// the others' beginnings and ends (16 tokens, 64 experts of 1024 x 2048: 79 us, with 20 KiB and two 90), and 24 rows of
+// activations at a time (16: 64 tokens, 4 of 32 experts of 2048 x 4096, 182 us, so 176; 32 tokens, 2 of 8 of 14336 x 4096, 318
+// and 294).  WIDE, for D, which has two rows for a token: 20 KiB and two, 32 rows at a time, where an expert has many tokens and
+// would have its weights read more often (64 tokens, us, narrow and wide: 2 of 8 of 14336 x 4096 386 and 353, 4 of 16 of 2048 x 4096 127
+// and 120, 4 of 32 177 and 182; G and U gain nothing by it: 357 and 126 for the first two).
 constexpr int NW = 4;
 template <bool WIDE> constexpr int WAVE_LDS = WIDE ? 20 * 1024 : 10 * 1024;
 template <bool WIDE> constexpr int WGS = WIDE ? 2 : 4;
@@ -267,15 +268,14 @@ __device__ __forceinline__ void expert_sums(u32x4_t buffer_w, const uint32_t (&w
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     char *const ring = s_ring + wave * WAVE_LDS<WIDE>;
     uint32_t at_w[4], at_x[XC];
-    int k_x[XC];  // the first input that the lane copies of activations
+    const int unit_0 = (lane & 15) ^ (lane >> 4);  // that the lane copies of activations, first of four copies
 #pragma unroll
     for (int g = 0; g < 4; g++)
         at_w[g] = w_at[g >> 1] + (uint32_t)((g & 1) * 8 + (lane >> 3)) * (uint32_t)n + 16 * ((lane & 7) ^ ((g & 1) * 4 + (lane >> 4)));
 #pragma unroll
     for (int g = 0; g < XC; g++) {
-        const int r = 4 * g + (lane >> 4), unit = (lane & 15) ^ (r & 15);
-        k_x[g] = r < rows ? 8 * unit : 1 << 30;
-        at_x[g] = r < rows ? x_at(r) + 16 * unit : 0u;
+        const int r = 4 * g + (lane >> 4);
+        at_x[g] = r < rows ? x_at(r) + 16 * (unit_0 ^ (4 * g & 15)) : 0xFFFFFF00u;
     }
     const int stages = (n + 127) / 128, mine = (stages - wave + NW - 1) / NW;
     auto copy = [&](int s, int slot) {
@@ -285,7 +285,7 @@ __device__ __forceinline__ void expert_sums(u32x4_t buffer_w, const uint32_t (&w
         // (behind a row's end: zeros, whatever the weights have there)
 #pragma unroll
         for (int g = 0; g < XC; g++)
-            copy_to_lds(buffer_x, (int)k + k_x[g] >= n ? 0xFFFFFF00u : at_x[g], 2 * k, ring + slot * STAGE + (4 + g) * 1024);
+            copy_to_lds(buffer_x, (int)k + 8 * (unit_0 ^ (4 * g & 15)) >= n ? 0xFFFFFF00u : at_x[g], 2 * k, ring + slot * STAGE + (4 + g) * 1024);
     };
 #pragma unroll
     for (int b = 0; b < 2; b++)
@@ -296,22 +296,22 @@ __device__ __forceinline__ void expert_sums(u32x4_t buffer_w, const uint32_t (&w
         const char *const stage = ring + slot * STAGE;
         i32x4_t w[2][2];
         op_t x[NB][4];
-#pragma unroll
-        for (int h = 0; h < 2; h++) {  // units hi and hi + 4: inputs 16 hi ... 16 hi + 15, and those 64 behind
+        auto weights = [&](int h) {  // units hi and hi + 4: inputs 16 hi ... 16 hi + 15, and those 64 behind
 #pragma unroll
             for (int b = 0; b < 2; b++)
                 w[b][h] = *reinterpret_cast<const i32x4_t *>(stage + b * 2048 + row * 128 + (((4 * h + hi) ^ (row >> 1)) << 4));
+        };
+        auto activations = [&](int h) {
 #pragma unroll
             for (int c = 0; c < NB; c++)
 #pragma unroll
-                for (int o = 0; o < 2; o++)
-                    x[c][2 * h + o] = *reinterpret_cast<const op_t *>(stage + 4096 + (XC < 4 ? row % (4 * XC) : 16 * c + row) * 256 +
-                                                                     (((8 * h + 2 * hi + o) ^ (XC < 4 ? row % (4 * XC) : row)) << 4));
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        again();
-#pragma unroll
-        for (int h = 0; h < 2; h++)
+                for (int o = 0; o < 2; o++) {
+                    // (the last rows again where there are no 16)
+                    const int r = 4 * XC - 16 * c < 16 ? row % (4 * XC - 16 * c) : row;
+                    x[c][2 * h + o] = *reinterpret_cast<const op_t *>(stage + 4096 + (16 * c + r) * 256 + (((8 * h + 2 * hi + o) ^ r) << 4));
+                }
+        };
+        auto multiply = [&](int h) {
 #pragma unroll
             for (int b = 0; b < 2; b++) {
                 op_t first, second;
@@ -322,6 +322,22 @@ __device__ __forceinline__ void expert_sums(u32x4_t buffer_w, const uint32_t (&w
                     sum[b][c] = Operand<T>::product(second, x[c][2 * h + 1], sum[b][c]);
                 }
             }
+        };
+        weights(0);
+        activations(0);
+        // (128 registers do not hold 24 rows' operands of a whole stage)
+        constexpr bool HALVES = XC == 6 && !WIDE;
+        if constexpr (HALVES) {
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        weights(1);
+        activations(1);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        again();
+        if constexpr (!HALVES) multiply(0);
+        multiply(1);
     };
 #pragma unroll
     for (int d = 0; d < D; d++)
@@ -356,12 +372,12 @@ __device__ __forceinline__ void expert_sums(u32x4_t buffer_w, const uint32_t (&w
     __syncthreads();
 }
 
-// All rows of activations, 16 or 32 at a time: done(block sums, number of the row) in the lanes that have a row.
+// All rows of activations, 24 or 32 at a time: done(block sums, number of the row) in the lanes that have a row.
 template <class T, bool WIDE, class At, class Done>
 __device__ __forceinline__ void expert_rows(u32x4_t buffer_w, const uint32_t (&w_at)[2], u32x4_t buffer_x, At x_at, int rows, int n,
                                             char *s_ring, Done done) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    for (int r0 = 0; r0 < rows; r0 += WIDE ? 32 : 16) {
+    for (int r0 = 0; r0 < rows; r0 += WIDE ? 32 : 24) {
         auto some = [&](auto xc) {
             float4_t sum[2][(xc + 3) / 4];
             expert_sums<T, xc, WIDE>(buffer_w, w_at, buffer_x, [&](int r) { return x_at(r0 + r); }, rows - r0, n, s_ring, sum);
@@ -370,7 +386,8 @@ __device__ __forceinline__ void expert_rows(u32x4_t buffer_w, const uint32_t (&w
         };
         if (rows - r0 <= 4) some(std::integral_constant<int, 1>{});
         else if (rows - r0 <= 8) some(std::integral_constant<int, 2>{});
-        else if (!WIDE || rows - r0 <= 16) some(std::integral_constant<int, 4>{});
+        else if (rows - r0 <= 16) some(std::integral_constant<int, 4>{});
+        else if (!WIDE || rows - r0 <= 24) some(std::integral_constant<int, 6>{});
         else if constexpr (WIDE) some(std::integral_constant<int, 8>{});
     }
 }
@@ -384,8 +401,8 @@ __device__ __forceinline__ int bit_of(uint64_t bits, int r) {
 // h of 16 rows of G and U of one expert.  CHOOSE, experts a lane of the choice: for as many tokens as there are waves, every workgroup makes the choice
 // itself, which takes less than a launch (1 token, 2 of 8 experts of 14336 x 4096: 78.3 us, with a launch 79.9), and the first
 // one writes it down.
-template <class T, int CHOOSE, bool WIDE> __global__ __launch_bounds__(NW * 64, WGS<WIDE>) void moe_up_kernel(MoeI8 a, Workspace ws) {
-    __shared__ __attribute__((aligned(1024))) char s_ring[NW * WAVE_LDS<WIDE>];
+template <class T, int CHOOSE> __global__ __launch_bounds__(NW * 64, WGS<false>) void moe_up_kernel(MoeI8 a, Workspace ws) {
+    __shared__ __attribute__((aligned(1024))) char s_ring[NW * WAVE_LDS<false>];
     const int u = blockIdx.y;
     const Plan *plan = ws.plan;
     if constexpr (CHOOSE > 0) {
@@ -404,7 +421,7 @@ template <class T, int CHOOSE, bool WIDE> __global__ __launch_bounds__(NW * 64, 
     const uint32_t w_at[2] = {(uint32_t)i0 * a.n, (uint32_t)(a.f + i0) * a.n};
     const float4_t sg = *reinterpret_cast<const float4_t *>(a.up_scale + (int64_t)e * 2 * a.f + i);
     const float4_t su = *reinterpret_cast<const float4_t *>(a.up_scale + (int64_t)e * 2 * a.f + a.f + i);
-    expert_rows<T, WIDE>(buffer_w, w_at, buffer_x, [&](int r) { return (uint32_t)bit_of(tokens, r) * (uint32_t)a.ldx * 2; }, count, a.n,
+    expert_rows<T, false>(buffer_w, w_at, buffer_x, [&](int r) { return (uint32_t)bit_of(tokens, r) * (uint32_t)a.ldx * 2; }, count, a.n,
                    s_ring, [&](float4_t g, float4_t up, int r, bool there) {
         if (!there) return;
         bf16x4_t high, low;
@@ -470,13 +487,12 @@ template <class T> void launch_moe(const MoeI8 &a, const Workspace &ws, hipStrea
     hipLaunchKernelGGL((moe_logits_kernel<T>), dim3(a.E, (a.T + 3) / 4), dim3(256), 0, st, a, ws.logits);
     const int experts = a.T * a.top_k < a.E ? a.T * a.top_k : a.E;
     if (a.T <= NW) {
-        if (a.E <= 64) hipLaunchKernelGGL((moe_up_kernel<T, 1, false>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
-        else hipLaunchKernelGGL((moe_up_kernel<T, MOST, false>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
+        if (a.E <= 64) hipLaunchKernelGGL((moe_up_kernel<T, 1>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
+        else hipLaunchKernelGGL((moe_up_kernel<T, MOST>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
     } else {
         if (a.E <= 64) hipLaunchKernelGGL((moe_choose_kernel<1>), dim3(1), dim3(1024), 0, st, a, ws);
         else hipLaunchKernelGGL((moe_choose_kernel<MOST>), dim3(1), dim3(1024), 0, st, a, ws);
-        if (wide(a)) hipLaunchKernelGGL((moe_up_kernel<T, 0, true>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
-        else hipLaunchKernelGGL((moe_up_kernel<T, 0, false>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
+        hipLaunchKernelGGL((moe_up_kernel<T, 0>), dim3(a.f / 16, experts), dim3(NW * 64), 0, st, a, ws);
     }
     if (wide(a)) hipLaunchKernelGGL((moe_down_kernel<true>), dim3((a.n + 31) / 32, experts), dim3(NW * 64), 0, st, a, ws);
     else hipLaunchKernelGGL((moe_down_kernel<false>), dim3((a.n + 31) / 32, experts), dim3(NW * 64), 0, st, a, ws);

@@ -125,6 +125,26 @@ def test_all_tokens_to_one_expert_and_one_token_each(q):
     layer.check()
 
 
+@pytest.mark.parametrize("T", [1, 4, 5, 8, 9, 12, 13, 16, 17, 20, 23, 24, 25, 28, 29, 32, 33, 40, 41, 47, 48, 49, 63, 64])
+def test_an_expert_with_so_many_tokens(q, T):
+    """All tokens choose expert 2 and one of the others, which then has about a third of them; many experts and few."""
+    import torch
+    for E, n, f in ((4, 272, 144), (40, 256, 128)):
+        layer = Layer(q, T, n, f, E, 2, "bf16" if T % 2 else "f16")
+        layer.bias = torch.zeros(E, device="cuda")
+        layer.bias[2] = 100.0
+        layer.call()
+        assert bool((layer.ids[:, 0] == 2).all())
+        layer.check()
+
+
+@pytest.mark.parametrize("T,E,top_k", [(1, 65, 2), (2, 256, 16), (3, 100, 5), (4, 128, 8), (4, 64, 16)])
+def test_few_tokens_and_many_experts(q, T, E, top_k):
+    layer = Layer(q, T, 128, 64, E, top_k, "bf16")
+    layer.call()
+    layer.check()
+
+
 def test_ties_go_to_the_lowest_expert(q):
     import torch
     for E in (8, 64, 130, 256):
