@@ -15,15 +15,26 @@ namespace qtip {
 
 namespace {
 
-// Whether and how rows are rotated: blocks of 1024 and more have all stages within a wave.
-enum Turn { NONE, SHORT_BLOCKS, LONG_BLOCKS };
+// Whether and how rows are rotated: blocks of 1024 and more have all stages within a wave.  Of short rows a workgroup of 256 lanes has
+// several, 16, 32 or 64 lanes a row, as they are (BY_) or rotated (TURN_).
+enum Turn { NONE, SHORT_BLOCKS, LONG_BLOCKS, BY_16, BY_32, BY_64, TURN_16, TURN_32, TURN_64 };
+constexpr bool rotated(Turn r) { return r == SHORT_BLOCKS || r == LONG_BLOCKS; }
+constexpr bool turned(Turn r) { return r == TURN_16 || r == TURN_32 || r == TURN_64; }
+constexpr int lanes_of(Turn r) {
+    return r == BY_16 || r == TURN_16 ? 16 : r == BY_32 || r == TURN_32 ? 32 : r == BY_64 || r == TURN_64 ? 64 : 0;
+}
 
 // Where a thread's quad number q lies in its row.  Rotated rows: a wave has 1024 neighbouring values (and, of rows above
 // 16384, 1024 more 16 waves on), a lane four quads of them 256 apart; which of 16 quads next to each other says rht_lane_t.
 template <Turn ROT> __device__ __forceinline__ int quad_in(int q) {
-    if constexpr (ROT != NONE) {
+    if constexpr (rotated(ROT)) {
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
         return 1024 * (wave + 16 * (q >> 2)) + 256 * (q & 3) + 64 * (lane >> 4) + 4 * rht_lane_t(lane & 15);
+    } else if constexpr (turned(ROT)) {
+        const int lane = threadIdx.x & (lanes_of(ROT) - 1);
+        return 64 * (lane >> 4) + 4 * rht_lane_t(lane & 15);
+    } else if constexpr (lanes_of(ROT) != 0) {
+        return 4 * (q * lanes_of(ROT) + ((int)threadIdx.x & (lanes_of(ROT) - 1)));
     } else {
         return 4 * (q * (int)blockDim.x + (int)threadIdx.x);
     }
@@ -33,8 +44,22 @@ struct Places {
     int base, first, second;
 };
 template <Turn ROT> __device__ __forceinline__ int quad_out(const Places &o, int q) {
-    if constexpr (ROT != NONE) return o.base + (q & 1 ? o.first : 0) + (q & 2 ? o.second : 0) + (q >> 2) * 16384;
-    else return quad_in<NONE>(q);
+    if constexpr (rotated(ROT)) return o.base + (q & 1 ? o.first : 0) + (q & 2 ? o.second : 0) + (q >> 2) * 16384;
+    else return quad_in<ROT>(q);
+}
+// The lane's row (past the last one, maybe, where a workgroup has several), and over the lanes that have it.
+template <Turn ROT> __device__ __forceinline__ int64_t row_of() {
+    if constexpr (lanes_of(ROT) == 0) return blockIdx.x;
+    else if constexpr (lanes_of(ROT) == 64) return (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    else return (int64_t)blockIdx.x * (256 / lanes_of(ROT)) + threadIdx.x / lanes_of(ROT);
+}
+template <Turn ROT> __device__ __forceinline__ float row_sum(float v, float *slots, int waves) {
+    if constexpr (lanes_of(ROT) != 0) return lanes_sum<lanes_of(ROT)>(v);
+    else return block_sum(v, slots, waves);
+}
+template <Turn ROT> __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t *slots, int waves) {
+    if constexpr (lanes_of(ROT) != 0) return lanes_max<lanes_of(ROT)>(v);
+    else return block_max(v, slots, waves);
 }
 
 // Four quads' butterflies over one bit of the quad's number.
@@ -152,6 +177,42 @@ template <Turn ROT> __device__ __forceinline__ Places rotate_quads(float4_t (&v)
     if (p == 13) return Places{quad + 2048 * (wave >> 2 & 1) + 1024 * (wave & ~7), 1024, 4096};
     return Places{quad + 1024 * (wave >> 2 & 3), 4096, 8192};
 }
+// The quad of a short row in place, blocks of at most 256: lane bits 4 and 5 by an exchange that brings each lane both sides.
+template <Turn ROT> __device__ __forceinline__ void rotate_quad(float4_t &v, const int8_t *__restrict__ signs, int n, int p) {
+    const int lane = threadIdx.x & 63, t = rht_lane_t(lane & 15), at = quad_in<ROT>(0);
+    const uint32_t s = at < n ? *reinterpret_cast<const uint32_t *>(signs + at) : 0u;
+    const float s1 = t & 1 ? -1.f : 1.f, s2 = t & 2 ? -1.f : 1.f, s4 = t & 4 ? -1.f : 1.f, s8 = t & 8 ? -1.f : 1.f;
+    const float4_t w = rht_signed(v, s);
+    const float a = w[0] + w[1], b = w[0] - w[1], c = w[2] + w[3], d = w[2] - w[3];
+    float x[4] = {a + c, b + d, a - c, b - d};
+    float scale = rht_scale(p) * s1 * s2;
+    QTIP_LANE_STAGE(x, s1, "quad_perm:[1,0,3,2]");
+    QTIP_LANE_STAGE(x, s2, "quad_perm:[2,3,0,1]");
+    if (p > 4) {
+        QTIP_LANE_STAGE(x, s4, "row_half_mirror");
+        scale *= s4;
+    }
+    if (p > 5) {
+        QTIP_LANE_STAGE(x, s8, "row_mirror");
+        scale *= s8;
+    }
+    typedef uint32_t two_t __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+        float y = x[r] * scale;
+        if (lanes_of(ROT) > 16 && p > 6) {
+            const two_t both = __builtin_bit_cast(two_t, __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, y), false, false));
+            const uint32_t one = both[0], two = both[1];
+            y = __builtin_bit_cast(float, one) + (lane & 16 ? -1.f : 1.f) * __builtin_bit_cast(float, two);
+        }
+        if (lanes_of(ROT) > 32 && p > 7) {
+            const two_t both = __builtin_bit_cast(two_t, __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, y), false, false));
+            const uint32_t one = both[0], two = both[1];
+            y = __builtin_bit_cast(float, one) + (lane & 32 ? -1.f : 1.f) * __builtin_bit_cast(float, two);
+        }
+        v[r] = y;
+    }
+}
 template <int Q, Turn ROT>
 __device__ __forceinline__ Places rotate_row(float4_t (&v)[Q], const int8_t *__restrict__ signs, int n, int p, float4_t *s_v) {
     Places o;
@@ -185,7 +246,7 @@ template <int Q, Turn ROT, bool RAGGED>
 __device__ __forceinline__ void store_i8(const float4_t (&v)[Q], const Places &o, int n, int8_t *__restrict__ to, float *scale, uint32_t top) {
     const float a = __builtin_bit_cast(float, top);
     const bool finite = top < 0x7F800000u;
-    if (threadIdx.x == 0) *scale = finite ? a / 127.f : __builtin_nanf("");
+    if (lanes_of(ROT) ? (threadIdx.x & (lanes_of(ROT) - 1)) == 0 : threadIdx.x == 0) *scale = finite ? a / 127.f : __builtin_nanf("");
     const float inverse = 127.f / a;
     // (127 / a overflows below 2^-121, and is 127 / 0 for a row of zeros)
     const bool plain = finite && a >= 0x1p-120f;
@@ -232,10 +293,11 @@ template <class T, int Q, Turn ROT, bool RAGGED> __device__ __forceinline__ void
 template <class T, int Q, Turn ROT, bool RAGGED>
 __global__ __launch_bounds__(1024) void quantize_rows_kernel(const T *__restrict__ x, const T *__restrict__ up, int n, int64_t ldx,
                                                              const int8_t *__restrict__ signs, int p, int8_t *__restrict__ out,
-                                                             int64_t ldq, float *__restrict__ scale) {
+                                                             int64_t ldq, float *__restrict__ scale, int rows) {
     extern __shared__ float4_t s_v[];  // 1024 floats a wave where a row is rotated over waves
     __shared__ uint32_t s_max[16];
-    const int64_t row = blockIdx.x;
+    const int64_t row = row_of<ROT>();
+    if (lanes_of(ROT) && row >= rows) return;
     typename Quad<T>::type raw[Q], raw_up[Q];
     load_row<T, Q, ROT, RAGGED>(raw, x + row * ldx, n);
     if (up) load_row<T, Q, ROT, RAGGED>(raw_up, up + row * ldx, n);
@@ -250,8 +312,9 @@ __global__ __launch_bounds__(1024) void quantize_rows_kernel(const T *__restrict
         }
     }
     Places o = {};
-    if constexpr (ROT != NONE) o = rotate_row<Q, ROT>(v, signs, n, p, s_v);
-    const uint32_t top = block_max(largest<Q, ROT>(v, o, n), s_max, blockDim.x >> 6);
+    if constexpr (rotated(ROT)) o = rotate_row<Q, ROT>(v, signs, n, p, s_v);
+    if constexpr (turned(ROT)) rotate_quad<ROT>(v[0], signs, n, p);
+    const uint32_t top = row_max<ROT>(largest<Q, ROT>(v, o, n), s_max, blockDim.x >> 6);
     store_i8<Q, ROT, RAGGED>(v, o, n, out + row * ldq, scale + row, top);
 }
 
@@ -262,7 +325,7 @@ __device__ __forceinline__ void normalize(float4_t (&v)[Q], int n, float over_n,
         float t = 0.f;
 #pragma unroll
         for (int q = 0; q < Q; q++) t += (v[q][0] + v[q][1]) + (v[q][2] + v[q][3]);
-        const float mean = block_sum(t, slots[0], waves) * over_n;
+        const float mean = row_sum<ROT>(t, slots[0], waves) * over_n;
 #pragma unroll
         for (int q = 0; q < Q; q++)
 #pragma unroll
@@ -271,7 +334,7 @@ __device__ __forceinline__ void normalize(float4_t (&v)[Q], int n, float over_n,
     float t = 0.f;
 #pragma unroll
     for (int q = 0; q < Q; q++) t += (v[q][0] * v[q][0] + v[q][1] * v[q][1]) + (v[q][2] * v[q][2] + v[q][3] * v[q][3]);
-    const float scale = 1.f / __builtin_sqrtf(block_sum(t, slots[1], waves) * over_n + eps);
+    const float scale = 1.f / __builtin_sqrtf(row_sum<ROT>(t, slots[1], waves) * over_n + eps);
 #pragma unroll
     for (int q = 0; q < Q; q++) v[q] *= scale;
 }
@@ -280,11 +343,12 @@ __device__ __forceinline__ void normalize(float4_t (&v)[Q], int n, float over_n,
 // too (1 x 4096 rotated, in a graph, 4.95 us and 4.34 so).  Many rows are bound by memory: 4096 x 8192 with a gate and 8-bit rows, 302 MB,
 // 66 us, 4.6 TB/s; 997 x 5003 with an fp32 residual, 60 MB, 17 us, 3.5 TB/s.
 template <class TY, class TH, int Q, Turn ROT, bool RAGGED, bool FEW>
-__global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a) {
+__global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a, int rows) {
     extern __shared__ float4_t s_v[];  // 1024 floats a wave where a row is rotated over waves
     __shared__ float s_sum[4][16];
     __shared__ uint32_t s_max[16];
-    const int64_t row = blockIdx.x;
+    const int64_t row = row_of<ROT>();
+    if (lanes_of(ROT) && row >= rows) return;
     const int n = a.n, waves = blockDim.x >> 6;
     const float over_n = 1.f / (float)n;
     typename Quad<TY>::type y[Q], g[Q];
@@ -356,9 +420,10 @@ __global__ __launch_bounds__(1024) void norm_residual_kernel(NormResidual a) {
         affine(pre, a.pre, a.pre_bias);
     }
     Places o = {};
-    if constexpr (ROT != NONE) o = rotate_row<Q, ROT>(v, a.signs, n, a.p, s_v);
+    if constexpr (rotated(ROT)) o = rotate_row<Q, ROT>(v, a.signs, n, a.p, s_v);
+    if constexpr (turned(ROT)) rotate_quad<ROT>(v[0], a.signs, n, a.p);
     if (a.x_type == TYPE_I8) {
-        const uint32_t top = block_max(largest<Q, ROT>(v, o, n), s_max, waves);
+        const uint32_t top = row_max<ROT>(largest<Q, ROT>(v, o, n), s_max, waves);
         store_i8<Q, ROT, RAGGED>(v, o, n, (int8_t *)a.x + row * a.ldx, a.x_scale + row, top);
     } else {
         store_row<Q, ROT, RAGGED>(v, o, n, a.x_type, a.x, row * a.ldx);
@@ -376,39 +441,52 @@ int log2_of(int block) {
 // Quads of a thread, then as many waves as hold the row.  One quad while there is at most a row for each CU (the shortest way
 // from load to store), else four: more rows on a CU at a time (us, one, two, four, eight quads: to 8 bits 4096 x 4096 13.6, 10.7,
 // 10.6, 10.3, norms 4096 x 8192 67.4, 67.4, 68.0, 108; 997 x 5003 20.5, 20.4, 17.2, 26.0; 4096 x 4096 33.3, 26.9, 29.1, 39.1).
-// Rotated rows: four quads, eight where 16 waves do not hold the row so.
+// Rotated rows: four quads, eight where 16 waves do not hold the row so.  Many rows of up to 512 values, rotated ones of up to 256:
+// several in a workgroup, with as few lanes as hold one (us, a workgroup a row and so: norms 131072 x 128 59.5 and 32.1, 65536 x 256
+// 44.4 and 35.2, 32768 x 512 32.7 and 30.0; to 8 bits 131072 x 64 31.2 and 7.6, 65536 x 256 17.2 and 12.7, 131072 x 128 in blocks of 128
+// 63.3 and 18.6).
 struct Shape {
-    int quads, waves, lds;
+    int quads, waves, lds, lanes;
+    int grid(int rows) const { return lanes ? (int)(((int64_t)rows + 256 / lanes - 1) / (256 / lanes)) : rows; }
 };
 static Shape shape_of(int rows, int n, int p) {
+    const int lanes = rows <= CUS || n > 512 ? 0 : n <= 64 ? 16 : n <= 128 ? 32 : 64;
+    if (lanes && n <= (p ? 256 : 512)) return {n <= 256 ? 1 : 2, 4, 0, lanes};
     if (p) {
         const int waves = n <= 16384 ? (n + 1023) / 1024 : 16;
-        return {n <= 16384 ? 4 : 8, waves, p > 10 ? waves * 4096 : 0};
+        return {n <= 16384 ? 4 : 8, waves, p > 10 ? waves * 4096 : 0, 0};
     }
     int quads = rows <= CUS ? 1 : 4;
     while (n > 4096 * quads) quads *= 2;
-    return {quads, (n + 256 * quads - 1) / (256 * quads), 0};
+    return {quads, (n + 256 * quads - 1) / (256 * quads), 0, 0};
 }
-#define QTIP_ROWS_BY_QUADS(LAUNCH, s, rot, ragged)  \
-    if (s.quads == 1) LAUNCH(1, rot, ragged);       \
-    else if (s.quads == 2) LAUNCH(2, rot, ragged);  \
-    else if (s.quads == 4) LAUNCH(4, rot, ragged);  \
-    else LAUNCH(8, rot, ragged)
-#define QTIP_ROWS_BY_SHAPE(LAUNCH, s, n, p)                               \
-    if (p >= 10 && s.quads == 4) { LAUNCH(4, LONG_BLOCKS, false); }       \
-    else if (p >= 10) { LAUNCH(8, LONG_BLOCKS, false); }                  \
-    else if (p && s.quads == 4) { LAUNCH(4, SHORT_BLOCKS, false); }       \
-    else if (p) { LAUNCH(8, SHORT_BLOCKS, false); }                       \
-    else if (n % 4) { QTIP_ROWS_BY_QUADS(LAUNCH, s, NONE, true); }        \
-    else { QTIP_ROWS_BY_QUADS(LAUNCH, s, NONE, false); }
+#define QTIP_ROWS_BY_QUADS(LAUNCH, s, ragged)              \
+    if (s.lanes == 16) LAUNCH(1, BY_16, ragged);           \
+    else if (s.lanes == 32) LAUNCH(1, BY_32, ragged);      \
+    else if (s.lanes && s.quads == 1) LAUNCH(1, BY_64, ragged); \
+    else if (s.lanes) LAUNCH(2, BY_64, ragged);            \
+    else if (s.quads == 1) LAUNCH(1, NONE, ragged);        \
+    else if (s.quads == 2) LAUNCH(2, NONE, ragged);        \
+    else if (s.quads == 4) LAUNCH(4, NONE, ragged);        \
+    else LAUNCH(8, NONE, ragged)
+#define QTIP_ROWS_BY_SHAPE(LAUNCH, s, n, p)                          \
+    if (p && s.lanes == 16) { LAUNCH(1, TURN_16, false); }           \
+    else if (p && s.lanes == 32) { LAUNCH(1, TURN_32, false); }      \
+    else if (p && s.lanes) { LAUNCH(1, TURN_64, false); }            \
+    else if (p >= 10 && s.quads == 4) { LAUNCH(4, LONG_BLOCKS, false); } \
+    else if (p >= 10) { LAUNCH(8, LONG_BLOCKS, false); }             \
+    else if (p && s.quads == 4) { LAUNCH(4, SHORT_BLOCKS, false); }  \
+    else if (p) { LAUNCH(8, SHORT_BLOCKS, false); }                  \
+    else if (n % 4) { QTIP_ROWS_BY_QUADS(LAUNCH, s, true); }         \
+    else { QTIP_ROWS_BY_QUADS(LAUNCH, s, false); }
 
 template <class T>
 static void launch_quantize(const void *x, const void *up, int rows, int n, int64_t ldx, const int8_t *signs, int p, int8_t *q,
                             int64_t ldq, float *scale, hipStream_t st) {
     const Shape s = shape_of(rows, n, p);
 #define QTIP_QUANTIZE(Q, ROT, RAGGED)                                                                                                 \
-    hipLaunchKernelGGL((quantize_rows_kernel<T, Q, ROT, RAGGED>), dim3(rows), dim3(s.waves * 64), s.lds, st, (const T *)x, (const T *)up, n, \
-                       ldx, signs, p, q, ldq, scale)
+    hipLaunchKernelGGL((quantize_rows_kernel<T, Q, ROT, RAGGED>), dim3(s.grid(rows)), dim3(s.waves * 64), s.lds, st, (const T *)x, (const T *)up, n, \
+                       ldx, signs, p, q, ldq, scale, rows)
     QTIP_ROWS_BY_SHAPE(QTIP_QUANTIZE, s, n, p);
 }
 
@@ -424,12 +502,12 @@ hipError_t launch_quantize_rows_i8(const void *x, const void *up, int type, int 
 template <class TY, class TH> static void launch_norm(const NormResidual &a, int rows, hipStream_t st) {
     const Shape s = shape_of(rows, a.n, a.p);
     if (a.p && rows <= CUS && a.n <= 8192) {
-        if (a.p >= 10) hipLaunchKernelGGL((norm_residual_kernel<TY, TH, 4, LONG_BLOCKS, false, true>), dim3(rows), dim3(s.waves * 64), s.lds, st, a);
-        else hipLaunchKernelGGL((norm_residual_kernel<TY, TH, 4, SHORT_BLOCKS, false, true>), dim3(rows), dim3(s.waves * 64), s.lds, st, a);
+        if (a.p >= 10) hipLaunchKernelGGL((norm_residual_kernel<TY, TH, 4, LONG_BLOCKS, false, true>), dim3(s.grid(rows)), dim3(s.waves * 64), s.lds, st, a, rows);
+        else hipLaunchKernelGGL((norm_residual_kernel<TY, TH, 4, SHORT_BLOCKS, false, true>), dim3(s.grid(rows)), dim3(s.waves * 64), s.lds, st, a, rows);
         return;
     }
 #define QTIP_NORM(Q, ROT, RAGGED) \
-    hipLaunchKernelGGL((norm_residual_kernel<TY, TH, Q, ROT, RAGGED, false>), dim3(rows), dim3(s.waves * 64), s.lds, st, a)
+    hipLaunchKernelGGL((norm_residual_kernel<TY, TH, Q, ROT, RAGGED, false>), dim3(s.grid(rows)), dim3(s.waves * 64), s.lds, st, a, rows)
     QTIP_ROWS_BY_SHAPE(QTIP_NORM, s, a.n, a.p);
 }
 

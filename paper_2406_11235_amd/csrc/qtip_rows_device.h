@@ -80,6 +80,33 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
     auto row = [&](int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); };
     return max(max(row(0), row(16)), max(row(32), row(48)));
 }
+// Over 16 or 32 neighbouring lanes, or a whole wave: each of them has it.
+template <int LANES> __device__ __forceinline__ float lanes_sum(float v) {
+    if constexpr (LANES == 64) return wave_sum(v);
+    auto add = [&](uint32_t o) { v += __builtin_bit_cast(float, o); };
+    add(dpp<0xB1>(__builtin_bit_cast(uint32_t, v)));
+    add(dpp<0x4E>(__builtin_bit_cast(uint32_t, v)));
+    add(dpp<0x141>(__builtin_bit_cast(uint32_t, v)));
+    add(dpp<0x140>(__builtin_bit_cast(uint32_t, v)));
+    if constexpr (LANES == 32) {
+        const auto both = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+        const uint32_t one = both[0], two = both[1];
+        v = __builtin_bit_cast(float, one) + __builtin_bit_cast(float, two);
+    }
+    return v;
+}
+template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+    if constexpr (LANES == 64) return wave_max(v);
+    v = max(v, dpp<0xB1>(v));
+    v = max(v, dpp<0x4E>(v));
+    v = max(v, dpp<0x141>(v));
+    v = max(v, dpp<0x140>(v));
+    if constexpr (LANES == 32) {
+        const auto both = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = max((uint32_t)both[0], (uint32_t)both[1]);
+    }
+    return v;
+}
 // Over the workgroup's waves, at most 16, which all make the call: every lane has it.  `slots`: 16 of them, that another exchange
 // may use once every wave has been at a barrier behind this call.
 __device__ __forceinline__ float block_sum(float v, float *slots, int waves) {
