@@ -46,7 +46,7 @@ SHAPES = [(1, 1, 0, 0, 0), (1, 3, 0, 5, 1), (2, 5, 0, 0, 0), (3, 2, 0, 1, 3), (6
           (16, 1, 16, 0, 0), (48, 3, 16, 8, 4), (96, 2, 32, 0, 0), (192, 2, 64, 0, 0), (384, 2, 128, 0, 0), (768, 3, 256, 0, 0),
           (1536, 2, 512, 0, 0), (1024, 700, 1024, 0, 0), (14336, 3, 2048, 0, 0), (28672, 2, 4096, 0, 0), (8192, 2, 8192, 0, 0),
           (24576, 2, 8192, 0, 0), (16384, 2, 16384, 0, 0), (32768, 2, 16384, 0, 0),
-          # few long rows are rotated in pieces; the last one of the first has no room for what pieces tell each other
+          # few long rows, rotated, that begin anywhere and end within a wave
           (20496, 3, 16, 1, 1), (20528, 3, 16, 1, 3), (28672, 40, 2048, 0, 0), (28672, 30, 1024, 5, 0), (18432, 2, 2048, 0, 1)]
 
 
